@@ -602,6 +602,83 @@ int qbp_xnor_gemm_bits(int64_t M, int64_t N, int64_t K, const uint32_t *A_bits, 
 int qbp_gated_xnor_gemm_bits(int64_t M, int64_t N, int64_t K, const uint32_t *nz_bits,
                              const uint32_t *sign_bits, const uint32_t *B_bits, int32_t *C, void *stream);
 
+/* ------------------------------------------------------------------------
+ * 8-bit floating-point products with a scale for each block of 128 (no
+ * counterpart in the paper, which quantises a tensor with one scale and an
+ * integer code: Section 4.  For tensors whose range one scale does not cover,
+ * the activations and gradients of language models among them).
+ *
+ * Codes are e4m3 (largest value 448) or e5m2 (57344), a byte each, laid out
+ * as the tensor they come from.  The scale of a block is a power of two 2^e: with
+ * amax its largest magnitude and V the format's largest value, e is the
+ * smallest integer >= -127 with amax <= V * 2^e (0 for a block of zeros);
+ * code = x * 2^-e rounded to nearest, ties to even.  So x / scale is exact,
+ * and codes and scales are reproducible bit for bit.  A block that holds an
+ * infinity or a NaN gets NaN codes and a NaN scale: every output that it
+ * enters is NaN.
+ *
+ * Scales.  To a product, an operand is outer indices (its rows or columns in
+ * the output) by reduction indices; a scale belongs to one outer index and
+ * the 128 reduction indices of a block.  It is the byte e + 127 (255: NaN),
+ * in pieces of 512 bytes for 128 outer indices and 4 blocks:
+ *   [ceil(outer / 128)][ceil(reduction / 512)][512],  the byte of outer index
+ *   r and block b at (r % 32) * 16 + (r / 32 % 4) * 4 + b % 4 of its piece
+ * -- qbp_f8_scale_bytes(outer, reduction) in all, 16-byte aligned.  Bytes
+ * behind the last index or block are 127.
+ *
+ * Real-valued tensors are fp32, bf16 or fp16 (qbp_dtype); all arithmetic is
+ * fp32, and a result is rounded once, as it is stored.  Every tensor is on
+ * the stream's device.
+ * ---------------------------------------------------------------------- */
+typedef enum { QBP_F32 = 0, QBP_BF16 = 1, QBP_F16 = 2 } qbp_dtype;
+enum { QBP_E4M3 = 0, QBP_E5M2 = 1 };
+
+size_t qbp_f8_scale_bytes(int64_t outer, int64_t reduction);
+
+/* x [rows x cols], the rows `ld` >= cols elements apart; cols a multiple of
+ * 16.  Two independent copies from one read of x, either may be left out
+ * (codes and scales both NULL):
+ *   q_rows, s_rows   blocks along the columns, for a product that reduces over
+ *                    the columns: outer = rows, reduction = cols
+ *   q_cols, s_cols   blocks along the rows, for a product that reduces over
+ *                    the rows: outer = cols, reduction = rows
+ * Codes are [rows x cols] dense in both, 16-byte aligned.  rows or cols of
+ * zero: nothing is done.  No workspace. */
+int qbp_quantize_f8(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int format,
+                    uint8_t *q_rows, uint8_t *s_rows, uint8_t *q_cols, uint8_t *s_cols, void *stream);
+
+/* One scale for each 128 x 128 block (weights): one copy of codes that serves
+ * products over the columns (s_rows) and over the rows (s_cols) alike; either
+ * table may be NULL, not both. */
+int qbp_quantize_f8_square(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int format,
+                           uint8_t *q, uint8_t *s_rows, uint8_t *s_cols, void *stream);
+
+/* out[m,n] = sum over blocks b of 2^(ea[m,b] + eb[n,b]) sum over k in b of
+ * A[m,k] B[k,n], accumulated in fp32 by the tensor cores, stored as out_dtype
+ * [M x N], dense, aligned to its element.  transA / transB as in qbp_gemm_s8: A is [M x K]
+ * (transA: stored [K x M]), B is [K x N] (transB: stored [N x K]); sA over
+ * outer = M, sB over outer = N, both over reduction = K.  An operand's innermost stored
+ * extent is a multiple of 16, the other extents are free; M or N of zero: nothing is done;
+ * K of zero: out is cleared.  The device status word is the start of `ws`, as
+ * for qbp_gemm_s8. */
+size_t qbp_gemm_f8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+int qbp_gemm_f8(int transA, int transB, int64_t M, int64_t N, int64_t K,
+                int formatA, const uint8_t *A, const uint8_t *sA,
+                int formatB, const uint8_t *B, const uint8_t *sB,
+                int out_dtype, void *out, void *ws, size_t ws_bytes, void *stream);
+
+/* A linear layer that serves: y [M x N] = x w^T with x [M x K] (rows ld
+ * apart) quantised here to e4m3 with blocks along K, and w [N x K] kept as
+ * codes (w_format) and scales over outer = N: qbp_quantize_f8 into the
+ * workspace and qbp_gemm_f8 in one call, with their results bit for bit.  y has x's type.
+ * K a multiple of 16. */
+size_t qbp_linear_f8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+int qbp_linear_f8(const void *x, int dtype, int64_t ld, int64_t M, int64_t N, int64_t K,
+                  int w_format, const uint8_t *w, const uint8_t *sw, void *y,
+                  void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,6 +20,8 @@ _LIB_PATH = Path(__file__).resolve().parent / "libqbp.so"
 QBP_PER_TENSOR, QBP_PER_CHANNEL = 0, 1
 QBP_ROUND_NEAREST, QBP_ROUND_STOCHASTIC = 0, 1
 QBP_CONV_FPROP, QBP_CONV_DGRAD = 0, 1
+QBP_F32, QBP_BF16, QBP_F16 = 0, 1, 2
+QBP_E4M3, QBP_E5M2 = 0, 1
 QBP_ERR_TIMEOUT = -6
 
 EXPORTS = (
@@ -37,6 +39,8 @@ EXPORTS = (
     "qbp_binarize_s8", "qbp_stc_ternarize_workspace_bytes", "qbp_stc_ternarize_s8",
     "qbp_tbp_weight_gradient_workspace_bytes", "qbp_tbp_weight_gradient",
     "qbp_pack_bits", "qbp_xnor_gemm_bits", "qbp_gated_xnor_gemm_bits",
+    "qbp_f8_scale_bytes", "qbp_quantize_f8", "qbp_quantize_f8_square", "qbp_gemm_f8_workspace_bytes", "qbp_gemm_f8",
+    "qbp_linear_f8_workspace_bytes", "qbp_linear_f8",
 )
 
 
@@ -94,6 +98,14 @@ def _load() -> C.CDLL:
     lib.qbp_layer_workspace_bytes.argtypes = [C.c_void_p]
     lib.qbp_range_chunked_workspace_bytes.argtypes = []
     lib.qbp_stc_ternarize_workspace_bytes.argtypes = []
+    i64, ptr, size = C.c_int64, C.c_void_p, C.c_size_t
+    lib.qbp_f8_scale_bytes.restype = size
+    lib.qbp_f8_scale_bytes.argtypes = [i64, i64]
+    lib.qbp_quantize_f8.argtypes = [ptr, C.c_int, i64, i64, i64, C.c_int, ptr, ptr, ptr, ptr, ptr]
+    lib.qbp_quantize_f8_square.argtypes = [ptr, C.c_int, i64, i64, i64, C.c_int, ptr, ptr, ptr, ptr]
+    lib.qbp_gemm_f8_workspace_bytes.argtypes = lib.qbp_linear_f8_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.qbp_gemm_f8.argtypes = [C.c_int, C.c_int, i64, i64, i64, C.c_int, ptr, ptr, C.c_int, ptr, ptr, C.c_int, ptr, ptr, size, ptr]
+    lib.qbp_linear_f8.argtypes = [ptr, C.c_int, i64, i64, i64, i64, C.c_int, ptr, ptr, ptr, ptr, size, ptr]
     lib.qbp_tbp_weight_gradient_workspace_bytes.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int64]
     return lib
 
@@ -421,6 +433,125 @@ def qbp_gated_xnor_gemm_bits(nz_bits, sign_bits, B_bits, K, out=None):
     _check(lib.qbp_gated_xnor_gemm_bits(C.c_int64(M), C.c_int64(N), C.c_int64(K), _ptr(nz_bits), _ptr(sign_bits), _ptr(B_bits),
                                         _ptr(out), _stream()))
     return out
+
+
+# ------------------------------------------- 8-bit floating point with a scale for each block of 128
+_DTYPES = {torch.float32: QBP_F32, torch.bfloat16: QBP_BF16, torch.float16: QBP_F16}
+
+
+def _dtype(t) -> int:
+    try:
+        return _DTYPES[t]
+    except KeyError:
+        raise TypeError(f"{t}: fp32, bf16 or fp16 is wanted") from None
+
+
+def _here(*tensors) -> int:
+    """The current device's index; every tensor given has to be on it (work is enqueued on its current stream)."""
+    index = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{index}")
+    return index
+
+
+def _rows_of(x):
+    """x as a matrix: (rows, columns, elements between rows).  Two dimensions may have padded rows, more have to be dense."""
+    if x.dim() == 2:
+        rows, cols = x.shape
+        if cols > 1 and x.stride(1) != 1:
+            raise ValueError("the innermost dimension has to be dense")
+        return rows, cols, x.stride(0) if rows > 1 else max(cols, 1)
+    if not x.is_contiguous():
+        raise ValueError("a tensor of other than two dimensions has to be contiguous")
+    cols = x.shape[-1] if x.dim() else 1
+    return (x.numel() // cols if cols else 0), cols, cols
+
+
+def _addr(t):
+    """Device address of a dense tensor (None: NULL)."""
+    if t is None: return None
+    if not t.is_contiguous(): raise ValueError("a dense tensor is wanted")
+    return t.data_ptr()
+
+
+def _codes(t):
+    """Device address of a tensor of 8-bit codes or scales."""
+    if t.element_size() != 1: raise TypeError(f"{t.dtype}: a tensor of bytes is wanted")
+    return _addr(t)
+
+
+def qbp_f8_scales(outer: int, reduction: int, device="cuda") -> torch.Tensor:
+    """Storage for the scales of an operand of `outer` rows (or columns) and `reduction` reduction indices."""
+    return torch.empty(lib.qbp_f8_scale_bytes(outer, reduction), dtype=torch.uint8, device=device)
+
+
+def qbp_f8_exponents(scales, outer: int, reduction: int) -> torch.Tensor:
+    """The scales' exponents as an int32 tensor [outer, blocks] (128: not a number), for looking at them."""
+    blocks = (reduction + 127) // 128
+    t = scales.view(-1, (blocks + 3) // 4, 32, 4, 4).permute(0, 3, 2, 1, 4).reshape(-1, (blocks + 3) // 4 * 4)
+    return t[:outer, :blocks].to(torch.int32) - 127
+
+
+def qbp_quantize_f8(x, format=QBP_E4M3, rows=True, cols=False):
+    """Codes and scales of x with blocks of 128 along its columns (rows=True: (q, s)), along its rows (cols=True), or
+    both from one read: (q_rows, s_rows, q_cols, s_cols).  x: [..., columns], fp32, bf16 or fp16."""
+    device = _here(x)
+    r, c, ld = _rows_of(x)
+    qr = sr = qc = sc = None
+    if rows: qr, sr = torch.empty(x.shape, dtype=torch.uint8, device=x.device), qbp_f8_scales(r, c, x.device)
+    if cols: qc, sc = torch.empty(x.shape, dtype=torch.uint8, device=x.device), qbp_f8_scales(c, r, x.device)
+    _check(lib.qbp_quantize_f8(x.data_ptr(), _dtype(x.dtype), r, c, ld, format, qr.data_ptr() if rows else None, sr.data_ptr() if rows else None,
+                               qc.data_ptr() if cols else None, sc.data_ptr() if cols else None, _stream_handle(device)))
+    return (qr, sr, qc, sc) if rows and cols else (qr, sr) if rows else (qc, sc)
+
+
+def qbp_quantize_f8_square(x, format=QBP_E4M3):
+    """Codes of x [rows, columns] with one scale for each 128 x 128 block, and the scales for products that reduce over the
+    columns and over the rows: (q, s_rows, s_cols)."""
+    device = _here(x)
+    r, c, ld = _rows_of(x)
+    q, sr, sc = torch.empty(x.shape, dtype=torch.uint8, device=x.device), qbp_f8_scales(r, c, x.device), qbp_f8_scales(c, r, x.device)
+    _check(lib.qbp_quantize_f8_square(x.data_ptr(), _dtype(x.dtype), r, c, ld, format, q.data_ptr(), sr.data_ptr(), sc.data_ptr(),
+                                      _stream_handle(device)))
+    return q, sr, sc
+
+
+def _scales_fit(s, outer, reduction, name):
+    if s.numel() != lib.qbp_f8_scale_bytes(outer, reduction):
+        raise ValueError(f"{name}: {s.numel()} bytes, scales of {outer} x {reduction} are {lib.qbp_f8_scale_bytes(outer, reduction)}")
+
+
+def qbp_gemm_f8(A, sA, B, sB, transA=False, transB=False, formatA=QBP_E4M3, formatB=QBP_E4M3, out_dtype=torch.float32, out=None, ws=None):
+    """The product of two tensors of codes: A [M, K] (transA: [K, M]), B [K, N] (transB: [N, K]), sA and sB their scales
+    over M and N by K.  Returns the fp32, bf16 or fp16 output [M, N]."""
+    device = _here(A, sA, B, sB, out, ws)
+    if transA: K, M = A.shape
+    else:      M, K = A.shape
+    N, kb = B.shape if transB else B.shape[::-1]
+    if kb != K: raise ValueError(f"the reduction is {K} in A and {kb} in B")
+    _scales_fit(sA, M, K, "sA"); _scales_fit(sB, N, K, "sB")
+    if out is None: out = torch.empty((M, N), dtype=out_dtype, device=A.device)
+    elif tuple(out.shape) != (M, N): raise ValueError(f"out is {tuple(out.shape)}, the product {(M, N)}")
+    if ws is None: ws = workspace(256, A.device)
+    _check(lib.qbp_gemm_f8(int(transA), int(transB), M, N, K, formatA, _codes(A), _codes(sA), formatB, _codes(B), _codes(sB), _dtype(out.dtype),
+                           _addr(out), ws.data_ptr(), ws.numel(), _stream_handle(device)))
+    return out
+
+
+def qbp_linear_f8(x, w, sw, w_format=QBP_E4M3, y=None, ws=None):
+    """y = x w^T of a layer that serves: x [..., K] real-valued, w [N, K] codes and sw their scales over N by K.  y has x's type."""
+    device = _here(x, w, sw, y, ws)
+    M, K, ld = _rows_of(x)
+    N, kw = w.shape
+    if kw != K: raise ValueError(f"x has {K} columns, w {kw}")
+    _scales_fit(sw, N, K, "sw")
+    if y is None: y = torch.empty((*x.shape[:-1], N), dtype=x.dtype, device=x.device)
+    elif tuple(y.shape) != (*x.shape[:-1], N) or y.dtype != x.dtype: raise ValueError(f"y is {tuple(y.shape)} {y.dtype}, the output {(*x.shape[:-1], N)} {x.dtype}")
+    if ws is None: ws = workspace(lib.qbp_linear_f8_workspace_bytes(M, N, K), x.device)
+    _check(lib.qbp_linear_f8(x.data_ptr(), _dtype(x.dtype), ld, M, N, K, w_format, _codes(w), _codes(sw), _addr(y), ws.data_ptr(), ws.numel(),
+                             _stream_handle(device)))
+    return y
 
 
 # ------------------------------------------------------------------- Range BN

@@ -1,0 +1,492 @@
+// 8-bit floating point with a scale for each block of 128: the quantisers, the product of a few output tiles on single CTAs,
+// and the entry points.  The scales' layout is described in qbp_f8.cuh; the product of many tiles runs on CTA pairs (qbp_f8_pair.cu).
+#include "qbp_f8.cuh"
+
+#include <algorithm>
+
+namespace qbp {
+
+// ================================================================== quantisers
+// A block takes one 128 x 128 tile: thread t holds the eight columns 8 (t % 16) of the rows t / 16 + 16 i in registers, so
+// that x is read once for both copies.  A row's largest magnitude is found by the sixteen lanes that hold it, a column's by a
+// warp's two rows and then across the warps in shared memory.  Magnitudes are compared as integers: that orders NaN above
+// infinity above the finite values, so that one comparison finds a block that is not finite.
+constexpr int kQuantThreads = 256;
+constexpr int kQuantPasses = 8;
+
+enum { kF8Rows = 1, kF8Cols = 2, kF8Square = 4 };
+
+// (the piece's byte of an outer index and a block)
+__device__ __forceinline__ int64_t scale_at(int64_t outer, int64_t block, int64_t groups)
+{
+    return ((outer >> 7) * groups + (block >> 2)) * kF8Piece + (outer & 31) * 16 + ((outer >> 5) & 3) * 4 + (block & 3);
+}
+// The byte of this outer index and block; behind the last block, the rest of its word.
+__device__ __forceinline__ void put_scale(uint8_t *s, int64_t outer, int64_t block, int64_t blocks, uint32_t byte)
+{
+    uint8_t *at = s + scale_at(outer, block, (blocks + 3) >> 2);
+    *at = (uint8_t)byte;
+    if (block == blocks - 1)
+        for (int k = (int)(block & 3) + 1; k < 4; ++k) *++at = 127;
+}
+
+template <typename T, int FORMAT, int WHAT>
+__global__ void __launch_bounds__(kQuantThreads) f8_quantize_kernel(const T *__restrict__ x, int64_t rows, int64_t cols, int64_t ld, int vec,
+                                                                    uint8_t *__restrict__ q_rows, uint8_t *__restrict__ s_rows,
+                                                                    uint8_t *__restrict__ q_cols, uint8_t *__restrict__ s_cols)
+{
+    __shared__ uint32_t s_amax[kQuantThreads / 32][kF8Block];
+    __shared__ uint8_t s_byte[kF8Block];
+    __shared__ uint32_t s_warp[kQuantThreads / 32];
+    const int lane16 = threadIdx.x & 15, high = threadIdx.x >> 4, warp = threadIdx.x >> 5;
+    const int64_t tile_c = blockIdx.x, tile_r = blockIdx.y;
+    const int64_t c0 = tile_c * kF8Block + 8 * lane16, r0 = tile_r * kF8Block;
+    const int n = (int)min((int64_t)8, max((int64_t)0, cols - c0));                // 8 or 0: cols is a multiple of 16
+    pdl_wait();
+    Raw8<T> raw[kQuantPasses];
+#pragma unroll
+    for (int i = 0; i < kQuantPasses; ++i) {
+        const int64_t r = r0 + 16 * i + high;
+        raw[i] = load8(x + (r < rows ? r : 0) * ld + (n ? c0 : 0), r < rows ? n : 0, vec != 0);
+    }
+    uint32_t col_max[8] = {}, tile_max = 0, row_max[kQuantPasses];
+#pragma unroll
+    for (int i = 0; i < kQuantPasses; ++i) {
+        float v[8];
+        unpack8(raw[i], v);
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t b = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+            m = max(m, b);
+            if (WHAT & kF8Cols) col_max[e] = max(col_max[e], b);
+        }
+        row_max[i] = m;
+        tile_max = max(tile_max, m);
+    }
+    const int64_t blocks_c = (cols + 127) >> 7, blocks_r = (rows + 127) >> 7;
+    uint32_t col_byte[8], tile_byte = 127;
+    if (WHAT & kF8Cols) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t m = max(col_max[e], __shfl_xor_sync(0xFFFFFFFFu, col_max[e], 16));
+            if ((threadIdx.x & 16) == 0) s_amax[warp][8 * lane16 + e] = m;
+        }
+        __syncthreads();
+        if (threadIdx.x < kF8Block) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int w = 0; w < kQuantThreads / 32; ++w) m = max(m, s_amax[w][threadIdx.x]);
+            const uint32_t byte = f8_scale_byte<FORMAT>(m);                        // (127 for columns behind the last)
+            s_byte[threadIdx.x] = (uint8_t)byte;
+            put_scale(s_cols, tile_c * kF8Block + threadIdx.x, tile_r, blocks_r, byte);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) col_byte[e] = s_byte[8 * lane16 + e];
+    }
+    if (WHAT & kF8Square) {
+        tile_max = __reduce_max_sync(0xFFFFFFFFu, tile_max);
+        if ((threadIdx.x & 31) == 0) s_warp[warp] = tile_max;
+        __syncthreads();
+        uint32_t m = 0;
+#pragma unroll
+        for (int w = 0; w < kQuantThreads / 32; ++w) m = max(m, s_warp[w]);
+        tile_byte = f8_scale_byte<FORMAT>(m);
+        if (threadIdx.x < kF8Block) {
+            const int64_t r = r0 + threadIdx.x, c = tile_c * kF8Block + threadIdx.x;
+            if (s_rows) put_scale(s_rows, r, tile_c, blocks_c, r < rows ? tile_byte : 127u);
+            if (s_cols) put_scale(s_cols, c, tile_r, blocks_r, c < cols ? tile_byte : 127u);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kQuantPasses; ++i) {
+        const int64_t r = r0 + 16 * i + high;
+        float v[8];
+        unpack8(raw[i], v);
+        uint32_t byte = tile_byte;
+        if (WHAT & kF8Rows) {
+            uint32_t m = row_max[i];
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+            byte = f8_scale_byte<FORMAT>(m);
+            if (lane16 == 0) put_scale(s_rows, r, tile_c, blocks_c, byte);           // (127 for rows behind the last)
+        }
+        if (r < rows && n) {
+            if (WHAT & (kF8Rows | kF8Square))
+                *reinterpret_cast<uint2 *>(q_rows + r * cols + c0) = f8_codes8<FORMAT>(v, f8_inverse(byte), byte == 255u);
+            if (WHAT & kF8Cols) {
+                float t[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) t[e] = __fmul_rn(v[e], f8_inverse(col_byte[e]));
+                uint2 c = f8_codes8<FORMAT>(t, 1.0f, false);
+                uint8_t *b = reinterpret_cast<uint8_t *>(&c);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (col_byte[e] == 255u) b[e] = (uint8_t)kF8Nan;
+                *reinterpret_cast<uint2 *>(q_cols + r * cols + c0) = c;
+            }
+        }
+    }
+}
+
+template <typename T, int FORMAT>
+static void launch_f8_quantize_as(const T *x, int64_t rows, int64_t cols, int64_t ld, int what, uint8_t *q_rows, uint8_t *s_rows, uint8_t *q_cols,
+                                  uint8_t *s_cols, cudaStream_t st)
+{
+    const dim3 grid((unsigned)f8_blocks(cols), (unsigned)f8_blocks(rows));
+    const int vec = aligned16(x) && ld * sizeof(T) % 16 == 0 ? 1 : 0;
+    auto *kernel = what == kF8Rows             ? f8_quantize_kernel<T, FORMAT, kF8Rows>
+                   : what == kF8Cols           ? f8_quantize_kernel<T, FORMAT, kF8Cols>
+                   : what == kF8Square         ? f8_quantize_kernel<T, FORMAT, kF8Square>
+                                               : f8_quantize_kernel<T, FORMAT, kF8Rows | kF8Cols>;
+    launch(kernel, grid, kQuantThreads, 0, st, x, rows, cols, ld, vec, q_rows, s_rows, q_cols, s_cols);
+}
+
+static int launch_f8_quantize(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int format, int what, uint8_t *q_rows,
+                              uint8_t *s_rows, uint8_t *q_cols, uint8_t *s_cols, cudaStream_t st)
+{
+    if (rows == 0 || cols == 0) return QBP_OK;
+    QBP_TRACE_BEGIN(st);
+    if (format == QBP_E4M3) QBP_FOR_DTYPE(dtype, T, (launch_f8_quantize_as<T, QBP_E4M3>((const T *)x, rows, cols, ld, what, q_rows, s_rows, q_cols, s_cols, st)));
+    else                    QBP_FOR_DTYPE(dtype, T, (launch_f8_quantize_as<T, QBP_E5M2>((const T *)x, rows, cols, ld, what, q_rows, s_rows, q_cols, s_cols, st)));
+    QBP_LAUNCH_OK("f8_quantize_kernel");
+    return QBP_OK;
+}
+
+// ============================================================ the split product
+// Few output tiles: a tile of 128 columns of the output by `bn` of its rows, its reduction split over the CTAs of a cluster.
+// The columns' operand (a layer's weights) is the 128-row side of the MMA and the rows (tokens, 16 to 128 of them) its N
+// side: a token or two then cost an N of 16 and not an M of 128, the accumulator's lanes are neighbouring outputs in memory,
+// and the weights, all that counts when rows are few, are read once, by as many SMs as there are tiles times pieces of the
+// reduction.  The CTAs of a cluster leave their fp32 partial tiles in shared memory and add up a share of the rows each, in the
+// order of the pieces.
+//
+// Roles: warp 0 loads by TMA, warp 1 copies scales to tensor memory and issues the MMAs, warps 2..5 take the accumulator out.
+// Every wait is bounded.
+constexpr int kSplitThreads = 192;
+constexpr int kSplitMaxStages = 10;
+constexpr int kSplitMaxParts = 8;
+constexpr uint32_t kSplitSmem = 220u * 1024u;
+constexpr uint32_t kSplitCols = 256;             // tensor memory: the accumulator in [0, 128), then four sets of 8 columns of scales
+constexpr int kSplitSets = 4;
+
+struct F8SplitParams {
+    CUtensorMap mapU, mapV, mapSU, mapSV;        // U: the output's columns (operand B), V: its rows (operand A)
+    OperandLayout u, v;
+    uint32_t idesc, stage_bytes;
+    int bn, stages, k_blocks, parts, clear;
+    int64_t M, N;
+    void *out; int dtype;
+    int *status;
+};
+
+template <typename T> __device__ __forceinline__ void split_store(void *out, int64_t at, float v) { static_cast<T *>(out)[at] = real_to<T>(v); }
+__device__ __forceinline__ void split_store(const F8SplitParams &P, int64_t at, float v)
+{
+    if (P.dtype == QBP_F32) split_store<float>(P.out, at, v);
+    else if (P.dtype == QBP_BF16) split_store<__nv_bfloat16>(P.out, at, v);
+    else split_store<__half>(P.out, at, v);
+}
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float load_of_cta(uint32_t smem_addr, uint32_t rank)
+{
+    uint32_t at; float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+
+__global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid_constant__ F8SplitParams P)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full_bar[kSplitMaxStages], empty_bar[kSplitMaxStages], acc_full;
+    __shared__ uint32_t tmem_slot;
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    uint8_t *smem = smem_raw + ((1024u - (raw_addr & 1023u)) & 1023u);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int part = (int)cluster_rank();
+    const int64_t n0 = (int64_t)(blockIdx.x / P.parts) * 128, m0 = (int64_t)blockIdx.y * P.bn;
+    const int kb0 = (int)((int64_t)P.k_blocks * part / P.parts), kb1 = (int)((int64_t)P.k_blocks * (part + 1) / P.parts);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < P.stages; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
+        mbar_init(&acc_full, 1);
+        mbar_fence_init();
+        tma_prefetch_desc(&P.mapU); tma_prefetch_desc(&P.mapV); tma_prefetch_desc(&P.mapSU); tma_prefetch_desc(&P.mapSV);
+    }
+    if (warp == 1) { tmem_alloc(&tmem_slot, kSplitCols); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    bool timed_out = false;
+    pdl_wait();
+    // The status word is cleared here and not by a launch of its own: a wait gives up a second after it began, long after the
+    // first block of a grid has started.
+    if (P.clear && threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) *P.status = 0;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t s = 0, ph = 1;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!mbar_wait(&empty_bar[s], ph)) { timed_out = true; break; }
+                uint8_t *su = smem + (size_t)s * P.stage_bytes, *sv = su + P.u.tile_bytes, *scales = sv + P.v.tile_bytes;
+                const bool with_scales = kb == kb0 || (kb & 3) == 0;
+                mbar_expect_tx(&full_bar[s], P.u.tile_bytes + P.v.tile_bytes + (with_scales ? 2u * kF8Piece : 0u));
+                if (P.u.major == 0) tma_load_2d(su, &P.mapU, &full_bar[s], kb * 128, (int)n0);
+                else                tma_load_2d(su, &P.mapU, &full_bar[s], (int)n0, kb * 128);
+                if (P.v.major == 0) tma_load_2d(sv, &P.mapV, &full_bar[s], kb * 128, (int)m0);
+                else                tma_load_2d(sv, &P.mapV, &full_bar[s], (int)m0, kb * 128);
+                if (with_scales) {
+                    tma_load_3d(scales, &P.mapSU, &full_bar[s], 0, kb >> 2, (int)(n0 >> 7));
+                    tma_load_3d(scales + kF8Piece, &P.mapSV, &full_bar[s], 0, kb >> 2, (int)(m0 >> 7));
+                }
+                if (++s == (uint32_t)P.stages) { s = 0; ph ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {
+        uint32_t s = 0, ph = 0, set = kSplitSets - 1;
+        for (int kb = kb0; kb < kb1; ++kb) {
+            if (!mbar_wait_uniform(&full_bar[s], ph)) { timed_out = true; break; }
+            tc_fence_after();
+            const uint32_t su = smem_u32(smem) + s * P.stage_bytes, sv = su + P.u.tile_bytes, scales = sv + P.v.tile_bytes;
+            if (kb == kb0 || (kb & 3) == 0) {
+                // (this set's last readers, the MMAs of at least 4 (kSplitSets - 1) + 1 blocks ago, are done: the stage of a
+                // later block than theirs has been filled again, at most kSplitMaxStages blocks ago)
+                set = set + 1 == kSplitSets ? 0u : set + 1;
+                if (elect_one()) {
+                    copy_piece(tmem + 128u + 8u * set, piece_desc(scales));
+                    copy_piece(tmem + 128u + 8u * set + 4u, piece_desc(scales + kF8Piece));
+                }
+            }
+            const uint32_t id = (uint32_t)(kb & 3), idesc = P.idesc | (id << 4) | (id << 29);
+            const uint32_t t_su = tmem + 128u + 8u * set, t_sv = t_su + 4u;
+            const uint32_t u_lo = ((su >> 4) & 0x3FFFu) | P.u.desc_lo, v_lo = ((sv >> 4) & 0x3FFFu) | P.v.desc_lo;
+#pragma unroll
+            for (uint32_t kk = 0; kk < 4; ++kk)
+                if (elect_one())
+                    mma_f8(tmem, ((uint64_t)P.u.desc_hi << 32) | (uint64_t)(u_lo + kk * P.u.kstep),
+                           ((uint64_t)P.v.desc_hi << 32) | (uint64_t)(v_lo + kk * P.v.kstep), idesc, t_su, t_sv, kb == kb0 && kk == 0 ? 0u : 1u);
+            if (elect_one()) mma_commit(&empty_bar[s]);
+            if (++s == (uint32_t)P.stages) { s = 0; ph ^= 1u; }
+        }
+        if (!timed_out && elect_one()) mma_commit(&acc_full);
+        __syncwarp();
+    }
+    const int quad = warp & 3;
+    const int64_t n = n0 + 32 * quad + lane;
+    float *mine = reinterpret_cast<float *>(smem);                 // partial sums [bn][128], where the ring was
+    if (warp >= 2) {
+        if (!mbar_wait_warp(&acc_full, 0)) timed_out = true;
+        tc_fence_after();
+        for (int c = 0; c < P.bn && !timed_out; c += 16) {
+            uint32_t r[16];
+            tmem_ld_32x16(tmem + ((uint32_t)(32 * quad) << 16) + (uint32_t)c, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                if (P.parts > 1) mine[(c + j) * 128 + 32 * quad + lane] = __uint_as_float(r[j]);
+                else if (n < P.N && m0 + c + j < P.M) split_store(P, (m0 + c + j) * P.N + n, __uint_as_float(r[j]));
+            }
+        }
+    }
+    if (timed_out) { raise_timeout(P.status); __nanosleep(1000000); }
+    tc_fence_before();
+    __syncthreads();
+    if (P.parts > 1) {
+        cluster_barrier();
+        if (warp >= 2 && n < P.N) {
+            const int64_t rows = min((int64_t)P.bn, P.M - m0);
+            for (int64_t j = rows * part / P.parts; j < rows * (part + 1) / P.parts; ++j) {
+                float sum = 0.0f;
+                for (int q = 0; q < P.parts; ++q) sum += load_of_cta(smem_u32(mine + j * 128 + 32 * quad + lane), (uint32_t)q);
+                split_store(P, (m0 + j) * P.N + n, sum);
+            }
+        }
+        __syncwarp();
+        cluster_barrier();                                            // nobody leaves while its partial sums are being read
+    }
+    if (warp == 1) { __syncwarp(); tmem_dealloc(tmem, kSplitCols); }
+}
+
+// A launch in clusters of `cluster` blocks, otherwise as launch().
+template <typename... P, typename... A>
+static void launch_clusters(void (*kernel)(P...), dim3 grid, unsigned cluster, unsigned threads, size_t smem, cudaStream_t st, A &&...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid; cfg.blockDim = dim3(threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = trace_is_on() ? 1 : 2;
+    (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
+static int launch_f8_split(const F8Product &p, cudaStream_t st)
+{
+    F8SplitParams P{};
+    int rc;
+    P.bn = p.transA || p.M > 64 ? 128 : p.M > 32 ? 64 : p.M > 16 ? 32 : 16;
+    if (p.transB) { P.u = layout_kmajor(128, 128);        rc = make_map_2d(&P.mapU, p.B, p.N, p.K, 128, 128); }
+    else          { P.u = layout_mnmajor(128, 128, 1, 0); rc = make_map_2d(&P.mapU, p.B, p.K, p.N, 128, 128); }
+    if (rc) return rc;
+    if (!p.transA) { P.v = layout_kmajor((uint32_t)P.bn, 128); rc = make_map_2d(&P.mapV, p.A, p.M, p.K, (uint32_t)P.bn, 128); }
+    else           { P.v = layout_mnmajor(128, 128, 1, 0);     rc = make_map_2d(&P.mapV, p.A, p.K, p.M, 128, 128); }
+    if (rc) return rc;
+    if ((rc = make_map_scales(&P.mapSU, p.sB, p.N, p.K, 1)) || (rc = make_map_scales(&P.mapSV, p.sA, p.M, p.K, 1))) return rc;
+    P.idesc = make_idesc_f8(p.formatB, p.formatA, P.u.major, P.v.major, 128, (uint32_t)P.bn);
+    P.k_blocks = (int)f8_blocks(p.K);
+    const int64_t tiles_n = f8_blocks(p.N), tiles_m = (p.M + P.bn - 1) / P.bn;
+    P.parts = 1;
+    while (P.parts < kSplitMaxParts && 2 * P.parts * tiles_n * tiles_m <= sm_count() && 4 * P.parts <= P.k_blocks) P.parts *= 2;
+    P.stage_bytes = (uint32_t)align_up(P.u.tile_bytes + P.v.tile_bytes + 2u * kF8Piece, 1024);
+    P.stages = (int)std::min<int64_t>(kSplitMaxStages, (kSplitSmem - 1024) / P.stage_bytes);
+    P.stages = std::min(P.stages, std::max(2, (P.k_blocks + P.parts - 1) / P.parts));
+    static_assert(kSplitMaxStages <= 4 * kSplitSets - 3, "a set of scales is written again while MMAs may read it");
+    const size_t ring = std::max<size_t>((size_t)P.stages * P.stage_bytes, P.parts > 1 ? (size_t)P.bn * 512 : 0);
+    P.M = p.M; P.N = p.N; P.out = p.out; P.dtype = p.dtype; P.status = p.status; P.clear = p.cleared ? 0 : 1;
+    static PerDeviceOnce configured;
+    QBP_SMEM_OPT_IN(configured, f8_split_kernel, kSplitSmem);
+    QBP_TRACE_BEGIN(st);
+    launch_clusters(f8_split_kernel, dim3((unsigned)(tiles_n * P.parts), (unsigned)tiles_m), (unsigned)P.parts, kSplitThreads, 1024 + ring, st, P);
+    QBP_LAUNCH_OK("f8_split_kernel");
+    return QBP_OK;
+}
+
+// ================================================================= entry points
+constexpr int64_t kF8MaxExtent = (int64_t)1 << 30;                  // TMA coordinates and the grid are 32-bit
+constexpr int64_t kF8MaxRowTiles = 65535;
+
+static int check_quantize(const char *name, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int format)
+{
+    if (!dtype_ok(dtype)) return fail(QBP_ERR_INVALID_ARG, "%s: dtype %d", name, dtype);
+    if (format != QBP_E4M3 && format != QBP_E5M2) return fail(QBP_ERR_INVALID_ARG, "%s: format %d", name, format);
+    if (rows < 0 || cols < 0 || ld < cols) return fail(QBP_ERR_INVALID_ARG, "%s: rows %lld, cols %lld, ld %lld", name, (long long)rows, (long long)cols, (long long)ld);
+    if (cols % 16) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: cols %lld is not a multiple of 16", name, (long long)cols);
+    if (f8_blocks(rows) > kF8MaxRowTiles || cols > kF8MaxExtent) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: %lld x %lld", name, (long long)rows, (long long)cols);
+    if (rows == 0 || cols == 0) return QBP_OK;
+    if (!x || !aligned_to(x, dtype_size(dtype))) return fail(QBP_ERR_INVALID_ARG, "%s: x is NULL or misaligned", name);
+    return QBP_OK;
+}
+
+extern "C" __attribute__((visibility("default"))) size_t qbp_f8_scale_bytes(int64_t outer, int64_t reduction)
+{
+    if (outer <= 0 || reduction <= 0) return 0;
+    return (size_t)(f8_blocks(outer) * f8_groups(reduction)) * kF8Piece;
+}
+
+extern "C" __attribute__((visibility("default"))) int qbp_quantize_f8(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int format,
+                                                                      uint8_t *q_rows, uint8_t *s_rows, uint8_t *q_cols, uint8_t *s_cols, void *stream)
+{
+    int rc = check_quantize("quantize_f8", x, dtype, rows, cols, ld, format);
+    if (rc) return rc;
+    if (!q_rows != !s_rows || !q_cols != !s_cols || (!q_rows && !q_cols)) return fail(QBP_ERR_INVALID_ARG, "quantize_f8: a copy needs both its codes and its scales");
+    if (!aligned16(q_rows) || !aligned16(s_rows) || !aligned16(q_cols) || !aligned16(s_cols)) return fail(QBP_ERR_INVALID_ARG, "quantize_f8: codes and scales start on 16-byte boundaries");
+    return launch_f8_quantize(x, dtype, rows, cols, ld, format, (q_rows ? kF8Rows : 0) | (q_cols ? kF8Cols : 0), q_rows, s_rows, q_cols, s_cols, (cudaStream_t)stream);
+}
+
+extern "C" __attribute__((visibility("default"))) int qbp_quantize_f8_square(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int format,
+                                                                             uint8_t *q, uint8_t *s_rows, uint8_t *s_cols, void *stream)
+{
+    int rc = check_quantize("quantize_f8_square", x, dtype, rows, cols, ld, format);
+    if (rc) return rc;
+    if (!q || (!s_rows && !s_cols)) return fail(QBP_ERR_INVALID_ARG, "quantize_f8_square: NULL codes, or neither table of scales");
+    if (!aligned16(q) || !aligned16(s_rows) || !aligned16(s_cols)) return fail(QBP_ERR_INVALID_ARG, "quantize_f8_square: codes and scales start on 16-byte boundaries");
+    return launch_f8_quantize(x, dtype, rows, cols, ld, format, kF8Square, q, s_rows, nullptr, s_cols, (cudaStream_t)stream);
+}
+
+static int run_product(const F8Product &p, cudaStream_t st)
+{
+    if (f8_pair_eligible(p)) return launch_f8_pair(p, st);
+    return launch_f8_split(p, st);
+}
+
+static int check_product(const F8Product &p, const char *name)
+{
+    if (!dtype_ok(p.dtype)) return fail(QBP_ERR_INVALID_ARG, "%s: dtype %d", name, p.dtype);
+    for (int f : {p.formatA, p.formatB})
+        if (f != QBP_E4M3 && f != QBP_E5M2) return fail(QBP_ERR_INVALID_ARG, "%s: format %d", name, f);
+    if (p.M < 0 || p.N < 0 || p.K < 0) return fail(QBP_ERR_INVALID_ARG, "%s: M %lld, N %lld, K %lld", name, (long long)p.M, (long long)p.N, (long long)p.K);
+    const int64_t inner_a = p.transA ? p.M : p.K, inner_b = p.transB ? p.K : p.N;
+    if (inner_a % 16 || inner_b % 16)
+        return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: the operands' innermost extents %lld and %lld are not multiples of 16", name, (long long)inner_a, (long long)inner_b);
+    if (p.M > kF8MaxExtent || p.N > kF8MaxExtent || p.K > kF8MaxExtent || (p.M + 127) / 128 > kF8MaxRowTiles)
+        return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: %lld x %lld x %lld", name, (long long)p.M, (long long)p.N, (long long)p.K);
+    return QBP_OK;
+}
+
+extern "C" __attribute__((visibility("default"))) size_t qbp_gemm_f8_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    (void)M; (void)N; (void)K;
+    return 256;                                                      // the status word
+}
+
+extern "C" __attribute__((visibility("default"))) int qbp_gemm_f8(int transA, int transB, int64_t M, int64_t N, int64_t K, int formatA, const uint8_t *A,
+                                                                  const uint8_t *sA, int formatB, const uint8_t *B, const uint8_t *sB, int out_dtype,
+                                                                  void *out, void *ws, size_t ws_bytes, void *stream)
+{
+    cudaStream_t st = (cudaStream_t)stream;
+    F8Product p{transA, transB, M, N, K, formatA, formatB, A, sA, B, sB, out, out_dtype, static_cast<int *>(ws), false};
+    int rc = check_product(p, "gemm_f8");
+    if (rc) return rc;
+    if (!ws || !aligned_to(ws, 256) || ws_bytes < qbp_gemm_f8_workspace_bytes(M, N, K))
+        return fail(QBP_ERR_WORKSPACE, "gemm_f8: workspace NULL, misaligned or smaller than %zu bytes", qbp_gemm_f8_workspace_bytes(M, N, K));
+    if (M == 0 || N == 0) { QBP_CUDA_OK(cudaMemsetAsync(ws, 0, 4, st)); return QBP_OK; }
+    if (!out || !aligned_to(out, dtype_size(out_dtype))) return fail(QBP_ERR_INVALID_ARG, "gemm_f8: out is NULL or misaligned");
+    if (K == 0) {
+        QBP_CUDA_OK(cudaMemsetAsync(ws, 0, 4, st));
+        QBP_CUDA_OK(cudaMemsetAsync(out, 0, (size_t)M * (size_t)N * dtype_size(out_dtype), st));
+        return QBP_OK;
+    }
+    for (const void *t : {(const void *)A, (const void *)sA, (const void *)B, (const void *)sB})
+        if (!t || !aligned16(t)) return fail(QBP_ERR_INVALID_ARG, "gemm_f8: an operand or its scales are NULL or not on a 16-byte boundary");
+    return run_product(p, st);
+}
+
+extern "C" __attribute__((visibility("default"))) size_t qbp_linear_f8_workspace_bytes(int64_t M, int64_t N, int64_t K)
+{
+    (void)N;
+    if (M <= 0 || K <= 0) return 256;
+    return 256 + align_up((size_t)M * (size_t)K, 256) + align_up(qbp_f8_scale_bytes(M, K), 256);
+}
+
+extern "C" __attribute__((visibility("default"))) int qbp_linear_f8(const void *x, int dtype, int64_t ld, int64_t M, int64_t N, int64_t K, int w_format,
+                                                                    const uint8_t *w, const uint8_t *sw, void *y, void *ws, size_t ws_bytes, void *stream)
+{
+    cudaStream_t st = (cudaStream_t)stream;
+    F8Product p{0, 1, M, N, K, QBP_E4M3, w_format, nullptr, nullptr, w, sw, y, dtype, static_cast<int *>(ws), false};
+    int rc = check_product(p, "linear_f8");
+    if (rc) return rc;
+    if ((rc = check_quantize("linear_f8", x, dtype, M, K, ld, QBP_E4M3))) return rc;
+    if (!ws || !aligned_to(ws, 256) || ws_bytes < qbp_linear_f8_workspace_bytes(M, N, K))
+        return fail(QBP_ERR_WORKSPACE, "linear_f8: workspace NULL, misaligned or smaller than %zu bytes", qbp_linear_f8_workspace_bytes(M, N, K));
+    if (M == 0 || N == 0) { QBP_CUDA_OK(cudaMemsetAsync(ws, 0, 4, st)); return QBP_OK; }
+    if (!y || !aligned_to(y, dtype_size(dtype))) return fail(QBP_ERR_INVALID_ARG, "linear_f8: y is NULL or misaligned");
+    if (K == 0) {
+        QBP_CUDA_OK(cudaMemsetAsync(ws, 0, 4, st));
+        QBP_CUDA_OK(cudaMemsetAsync(y, 0, (size_t)M * (size_t)N * dtype_size(dtype), st));
+        return QBP_OK;
+    }
+    if (!w || !sw || !aligned16(w) || !aligned16(sw)) return fail(QBP_ERR_INVALID_ARG, "linear_f8: the weights or their scales are NULL or not on a 16-byte boundary");
+    WsCarver c(ws, ws_bytes);
+    c.take<int>(1);
+    uint8_t *q = c.take<uint8_t>((size_t)M * (size_t)K), *s = c.take<uint8_t>(qbp_f8_scale_bytes(M, K));
+    if ((rc = launch_f8_quantize(x, dtype, M, K, ld, QBP_E4M3, kF8Rows, q, s, nullptr, nullptr, st))) return rc;
+    p.A = q; p.sA = s;
+    return run_product(p, st);
+}
+
+}  // namespace qbp

@@ -18,6 +18,7 @@
 //   acc = raw + rowterm[m] + colterm[class(m)][n]
 // where, for a convolution, class(m) says which taps of output pixel m fall
 // inside the image (real-zero padding contributes nothing).
+#include "qbp_f8.cuh"
 #include "qbp_mma.cuh"
 #include "qbp_sums.cuh"
 
@@ -113,6 +114,41 @@ int make_map_out_nhwc(CUtensorMap *map, float *base, uint64_t N, uint64_t H, uin
     CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(QBP_ERR_CUDA, "cuTensorMapEncodeTiled(fp32 nhwc output) failed: %d", (int)r);
+    return QBP_OK;
+}
+
+// Scales of 8-bit floating-point codes: pieces of 128 words, groups of four blocks of the reduction, tiles of 128 outer indices.
+int make_map_scales(CUtensorMap *map, const void *base, uint64_t outer, uint64_t K, uint32_t tiles)
+{
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return fail(QBP_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+    const cuuint64_t groups = (K + 511) / 512;
+    cuuint64_t dims[3] = {128, groups, (outer + 127) / 128};
+    cuuint64_t strides[2] = {512, 512 * groups};
+    cuuint32_t box[3] = {128, 1, tiles};
+    cuuint32_t estr[3] = {1, 1, 1};
+    CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(QBP_ERR_CUDA, "cuTensorMapEncodeTiled(scales of %llu x %llu) failed: %d", (unsigned long long)outer,
+                                       (unsigned long long)K, (int)r);
+    return QBP_OK;
+}
+
+// Output matrix of any real type [rows x cols] stored in boxes of 32 rows x 32 columns: rows of 128 or 64 bytes, swizzled alike.
+int make_map_out_32(CUtensorMap *map, void *base, uint64_t rows, uint64_t cols, int dtype)
+{
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return fail(QBP_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+    const bool wide = dtype == QBP_F32;
+    cuuint64_t dims[2] = {cols, rows};
+    cuuint64_t strides[1] = {cols * (wide ? 4 : 2)};
+    cuuint32_t box[2] = {32, 32};
+    cuuint32_t estr[2] = {1, 1};
+    CUresult r = enc(map, wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == QBP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                     2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, wide ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                     CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(QBP_ERR_CUDA, "cuTensorMapEncodeTiled(output %llu x %llu) failed: %d", (unsigned long long)rows,
+                                       (unsigned long long)cols, (int)r);
     return QBP_OK;
 }
 
