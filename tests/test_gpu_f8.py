@@ -183,3 +183,31 @@ def test_products(B, M, N, K, transA, transB):
         if dtype == "float16" and np.abs(a @ b.T).max() > 60000: continue
         check_product(got, a, b, K, dtype)
     assert B.status_word(B.workspace(256)) == 0
+
+
+def check_on_device(got, a, b, K, dtype):
+    """check_product with the 64-bit products taken on the device."""
+    import torch
+    a, b = torch.from_numpy(a).cuda(), torch.from_numpy(np.ascontiguousarray(b)).cuda()
+    want = a @ b.T
+    size = a.abs() @ b.abs().T
+    tol = (2 * -(-K // 32) + 8) * 2.0 ** -23 * size
+    tol = tol + half_step(dtype) * (want.abs() + tol)
+    assert bool(((got.double() - want).abs() <= tol).all())
+
+
+# more output tiles than the device has pairs of SMs, several rounds of them, ragged in every direction; an odd number of columns
+# (rows that start off a 16-byte boundary); a reduction of one block and of many
+@pytest.mark.parametrize("M,N,K,transA,transB", [(2600, 2100, 640, False, True), (5000, 4208, 272, False, False), (4112, 4000, 1003, True, False),
+                                                 (2704, 2563, 400, True, True), (9000, 1001, 128, False, True), (2048, 2560, 2048, False, True),
+                                                 (70000, 144, 256, False, False), (260, 40000, 144, False, True)])
+def test_products_of_many_tiles(B, M, N, K, transA, transB):
+    import torch
+    qa, sa, a = operand(B, M, K, transA, 0, M + 1)
+    qb, sb, b = operand(B, N, K, not transB, 1, N + 2)
+    for dtype in ("float32", "bfloat16"):
+        got = B.qbp_gemm_f8(qa, sa, qb, sb, transA=transA, transB=transB, formatB=1, out_dtype=getattr(torch, dtype))
+        check_on_device(got, a, b, K, dtype)
+    again = B.qbp_gemm_f8(qa, sa, qb, sb, transA=transA, transB=transB, formatB=1, out_dtype=torch.bfloat16)
+    assert torch.equal(again, got)                                # the same bits every time
+    assert B.status_word(B.workspace(256)) == 0
