@@ -679,6 +679,65 @@ int qbp_linear_f8(const void *x, int dtype, int64_t ld, int64_t M, int64_t N, in
                   int w_format, const uint8_t *w, const uint8_t *sw, void *y,
                   void *ws, size_t ws_bytes, void *stream);
 
+/* ------------------------------------------------------------------------
+ * The join between two blocks of a residual network (no counterpart in the
+ * paper, whose networks join convolutions by Range BN): the norm after a
+ * block, its gate, dropout, the residual stream and the norm before the next block in
+ * one pass over the rows.  With RMS(v) = sqrt(mean of v^2 over the row + eps),
+ * of block output b and residual stream x, [rows x cols] each, dense:
+ *   n = b / RMS(b) * w_post           (post != 0; else n = b)
+ *   d = dropout(n)                    (p > 0; see qbp_dropout; else d = n)
+ *   r = alpha * x + gate * d          rounded to x's type as it is stored
+ *   h = r / RMS(r) * w_pre            (pre != 0) from the rounded r
+ * gate [gates x cols]: row i takes gate row i / gate_rows (gate_rows = 0: one
+ * gate row for all; gates = ceil(rows / gate_rows)).  w_post, w_pre, gate
+ * (each nullable: ones) are fp32.  b == NULL (post and p then 0, gate NULL): the norm before a
+ * first block, r = alpha * x; r may be NULL then if alpha is 1, and h is made from x.
+ * x and r have x_dtype, b and h b_dtype; rows of any number, cols up to
+ * QBP_RESNORM_MAX_COLS, every tensor aligned to its element (16 bytes and cols a multiple of 8:
+ * faster).  rstd_post / rstd_pre [rows] (nullable) receive 1 / RMS for the backward pass.
+ * r may be x, and h may be b.
+ * ---------------------------------------------------------------------- */
+#define QBP_RESNORM_MAX_COLS 16384
+typedef struct {
+    int64_t rows, cols;
+    int32_t x_dtype, b_dtype;
+    int32_t post, pre;             /* whether there is a norm after / before    */
+    float eps, alpha;
+    int64_t gate_rows;
+    float p;                       /* dropout, 0 <= p <= 1                      */
+    uint32_t tensor_id;
+    uint64_t seed, index_base;     /* element (i, j) is number index_base + i * cols + j */
+} qbp_resnorm_desc;
+
+int qbp_resnorm_fwd(const qbp_resnorm_desc *d, const void *x, const void *b, const float *w_post, const float *gate,
+                    const float *w_pre, void *r, void *h, float *rstd_post, float *rstd_pre, void *stream);
+
+/* Its gradients, from those of r and h (dr in x's type, nullable: nothing else uses r;
+ * dh in b's type, wanted with pre):
+ *   R = dr + dh w_pre rstd_pre - r rstd_pre^3 mean(dh w_pre r)       the whole gradient at r
+ *   dx = alpha R;  dgate = sum of R d over the gate's rows
+ *   v = gate R dropout'(.);  dw_post = sum over the rows of v b rstd_post
+ *   db = v w_post rstd_post - b rstd_post^3 mean(v w_post b)         (without post: db = v)
+ *   dw_pre = sum over the rows of dh r rstd_pre
+ * b, r, rstd_* as the forward had and left them.  dx, db and the fp32 sums dw_post, dgate
+ * [gates x cols], dw_pre are each nullable; sums are fp32 in a fixed order.  dx may be dr, and db may be dh. */
+size_t qbp_resnorm_bwd_workspace_bytes(const qbp_resnorm_desc *d);
+
+int qbp_resnorm_bwd(const qbp_resnorm_desc *d, const void *dr, const void *dh, const void *b, const void *r,
+                    const float *rstd_post, const float *rstd_pre, const float *w_post, const float *gate, const float *w_pre,
+                    void *dx, void *db, float *dw_post, float *dgate, float *dw_pre, void *ws, size_t ws_bytes, void *stream);
+
+/* Dropout: y[i] = x[i] * 65536 / (65536 - t) where the draw of element index_base + i is
+ * at least t = floor(p * 65536 + 1/2), else 0 (whatever x[i] is; t = 65536: all of them).  The mask is
+ * never stored: the backward pass is the same call on the gradient.  Draws are 16 bits of a
+ * Philox4x32-10 word, eight to a block: key = seed, counter = (i/8 low, i/8 high, tensor_id,
+ * 0xFFFFFFFF), word (i / 2) % 4, its low half for even i (the stochastic quantisers'
+ * counters end in other words: equal ids do not correlate).  n elements of the type, any
+ * alignment of their type; y may be x; index_base a multiple of 8. */
+int qbp_dropout(const void *x, int dtype, int64_t n, float p, uint64_t seed, uint32_t tensor_id, uint64_t index_base,
+                void *y, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

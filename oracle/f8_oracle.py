@@ -89,3 +89,74 @@ def values(q, fmt, ex_full):
 def spread(ex, n, axis=1):
     """Exponents of blocks of 128 along `axis`, one for each of n elements."""
     return np.take(np.repeat(ex, 128, axis), np.arange(n), axis)
+
+
+# --------------------------------------------------------------- dropout
+def philox(counter, key):
+    """Philox4x32-10 of counters [n, 4] (uint32 values) and a 64-bit key."""
+    low = np.uint64(0xFFFFFFFF)
+    c = [counter[:, k].astype(np.uint64) for k in range(4)]
+    k0, k1 = key & 0xFFFFFFFF, key >> 32
+    for _ in range(10):
+        a, b = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(b >> np.uint64(32)) ^ c[1] ^ np.uint64(k0), b & low, (a >> np.uint64(32)) ^ c[3] ^ np.uint64(k1), a & low]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    return np.stack(c, 1).astype(np.uint32)
+
+
+def draws(first, count, seed, tensor_id):
+    """The 16-bit draws of elements first .. first + count - 1."""
+    i = np.arange(first, first + count, dtype=np.uint64)
+    block = i >> np.uint64(3)
+    counter = np.stack([block & np.uint64(0xFFFFFFFF), block >> np.uint64(32), np.full_like(i, tensor_id), np.full_like(i, 0xFFFFFFFF)], 1)
+    w = philox(counter, seed)
+    k = (i % np.uint64(8)).astype(np.int64)
+    return (w[np.arange(count), k // 2] >> (16 * (k % 2)).astype(np.uint32)) & np.uint32(0xFFFF)
+
+
+def keep(shape, p, seed, tensor_id, index_base=0):
+    """The factor of each element: 1 / (1 - p) with p in steps of 2^-16, or 0."""
+    t = int(np.floor(float(np.float32(p)) * 65536 + 0.5))
+    n = int(np.prod(shape))
+    if t == 65536:
+        return np.zeros(shape)
+    return np.where(draws(index_base, n, seed, tensor_id) >= t, 65536.0 / (65536 - t), 0.0).reshape(shape)
+
+
+# --------------------------------------------------------------- the join of two blocks
+def join(x, b, w_post, gate, w_pre, alpha, eps, gate_rows, mask, store, post=True, pre=True):
+    """r (before and after `store` rounds it), h and both 1 / RMS, in 64 bits."""
+    rows, c = x.shape
+    ones = np.ones(c)
+    g = np.ones((rows, c)) if gate is None else gate[np.arange(rows) // gate_rows if gate_rows else np.zeros(rows, int)]
+    w1, w2 = ones if w_post is None else w_post, ones if w_pre is None else w_pre
+    q1 = 1 / np.sqrt((b * b).mean(1) + eps) if post else np.ones(rows)
+    n = b * q1[:, None] * w1 if post else b
+    exact = alpha * x + g * np.where(mask != 0, n * mask, 0.0)
+    r = store(exact)
+    q2 = 1 / np.sqrt((r * r).mean(1) + eps)
+    return exact, r, r * q2[:, None] * w2 if pre else None, q1, q2
+
+
+def join_gradients(dr, dh, b, r, q1, q2, w_post, gate, w_pre, alpha, gate_rows, mask, post=True, pre=True):
+    """(dx, db, dw_post, dgate, dw_pre) by the chain rule, in 64 bits."""
+    rows, c = b.shape
+    ones = np.ones(c)
+    at = np.arange(rows) // gate_rows if gate_rows else np.zeros(rows, int)
+    g = np.ones((rows, c)) if gate is None else gate[at]
+    w1, w2 = ones if w_post is None or not post else w_post, ones if w_pre is None else w_pre
+    R = np.zeros_like(b) if dr is None else dr.copy()
+    dw2 = None
+    if pre:
+        rh = r * q2[:, None]
+        u = dh * w2
+        R = R + q2[:, None] * (u - rh * (u * rh).mean(1, keepdims=True))
+        dw2 = (dh * rh).sum(0)
+    bh = b * q1[:, None] if post else b
+    live = np.where(mask != 0, R, 0.0)
+    v = live * g * mask
+    dg = np.zeros((at.max() + 1, c))
+    np.add.at(dg, at, live * mask * bh * w1)
+    z = v * w1
+    db = q1[:, None] * (z - bh * (z * bh).mean(1, keepdims=True)) if post else v
+    return alpha * R, db, (v * bh).sum(0) if post else None, dg, dw2

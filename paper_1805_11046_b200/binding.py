@@ -41,6 +41,7 @@ EXPORTS = (
     "qbp_pack_bits", "qbp_xnor_gemm_bits", "qbp_gated_xnor_gemm_bits",
     "qbp_f8_scale_bytes", "qbp_quantize_f8", "qbp_quantize_f8_square", "qbp_gemm_f8_workspace_bytes", "qbp_gemm_f8",
     "qbp_linear_f8_workspace_bytes", "qbp_linear_f8",
+    "qbp_resnorm_fwd", "qbp_resnorm_bwd_workspace_bytes", "qbp_resnorm_bwd", "qbp_dropout",
 )
 
 
@@ -71,6 +72,13 @@ class Requant(C.Structure):
     """qbp_requant: where a pass writes the 8-bit codes of the activation it produces (q, qp) and, optionally,
     each row's code sum."""
     _fields_ = [("q", C.c_void_p), ("qp", C.c_void_p), ("row_sums", C.c_void_p), ("chan_sums", C.c_void_p)]
+
+
+class ResnormDesc(C.Structure):
+    """qbp_resnorm_desc: see resnorm_desc()."""
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("x_dtype", C.c_int32), ("b_dtype", C.c_int32), ("post", C.c_int32),
+                ("pre", C.c_int32), ("eps", C.c_float), ("alpha", C.c_float), ("gate_rows", C.c_int64), ("p", C.c_float),
+                ("tensor_id", C.c_uint32), ("seed", C.c_uint64), ("index_base", C.c_uint64)]
 
 
 def requant(q, qp, row_sums=None, chan_sums=None) -> Requant:
@@ -106,6 +114,10 @@ def _load() -> C.CDLL:
     lib.qbp_gemm_f8_workspace_bytes.argtypes = lib.qbp_linear_f8_workspace_bytes.argtypes = [i64, i64, i64]
     lib.qbp_gemm_f8.argtypes = [C.c_int, C.c_int, i64, i64, i64, C.c_int, ptr, ptr, C.c_int, ptr, ptr, C.c_int, ptr, ptr, size, ptr]
     lib.qbp_linear_f8.argtypes = [ptr, C.c_int, i64, i64, i64, i64, C.c_int, ptr, ptr, ptr, ptr, size, ptr]
+    lib.qbp_resnorm_fwd.argtypes = [ptr] * 11
+    lib.qbp_resnorm_bwd_workspace_bytes.argtypes = [ptr]
+    lib.qbp_resnorm_bwd.argtypes = [ptr] * 16 + [size, ptr]
+    lib.qbp_dropout.argtypes = [ptr, C.c_int, i64, C.c_float, C.c_uint64, C.c_uint32, C.c_uint64, ptr, ptr]
     lib.qbp_tbp_weight_gradient_workspace_bytes.argtypes = [C.c_void_p, C.c_int64, C.c_int64, C.c_int64]
     return lib
 
@@ -551,6 +563,79 @@ def qbp_linear_f8(x, w, sw, w_format=QBP_E4M3, y=None, ws=None):
     if ws is None: ws = workspace(lib.qbp_linear_f8_workspace_bytes(M, N, K), x.device)
     _check(lib.qbp_linear_f8(x.data_ptr(), _dtype(x.dtype), ld, M, N, K, w_format, _codes(w), _codes(sw), _addr(y), ws.data_ptr(), ws.numel(),
                              _stream_handle(device)))
+    return y
+
+
+# ------------------------------------------- the join between two blocks, and dropout
+QBP_RESNORM_MAX_COLS = 16384
+
+
+def resnorm_desc(x, b=None, alpha=1.0, eps=1e-6, gate_rows=0, p=0.0, seed=0, tensor_id=0, index_base=0, post=None, pre=True) -> ResnormDesc:
+    """The join of the residual stream x [..., columns] with a block's output b: r = alpha x + gate * dropout(norm(b) w_post),
+    h = norm(r) w_pre.  post / pre: whether there is a norm after the block (by default with b) and before the next one;
+    gate_rows: rows that share a row of the gate (0: all); p, seed, tensor_id, index_base: the dropout's, as in qbp_dropout."""
+    cols = x.shape[-1]
+    return ResnormDesc(x.numel() // cols if cols else 0, cols, _dtype(x.dtype), _dtype((x if b is None else b).dtype), int(b is not None if post is None else post),
+                       int(pre), eps, alpha, gate_rows, p, tensor_id, seed, index_base)
+
+
+def _real(t, count, dtype, name):
+    """Device address of a dense real-valued tensor of `count` elements and this qbp_dtype (None: NULL)."""
+    if t is None: return None
+    if _DTYPES.get(t.dtype) != dtype: raise TypeError(f"{name}: {t.dtype} is not the descriptor's type")
+    if t.numel() != count: raise ValueError(f"{name}: {t.numel()} elements, {count} are wanted")
+    return _addr(t)
+
+
+def _gates(d) -> int:
+    return -(-d.rows // d.gate_rows) if d.gate_rows else 1
+
+
+def qbp_resnorm_fwd(d: ResnormDesc, x, b=None, w_post=None, gate=None, w_pre=None, r=None, h=None, rstd_post=None, rstd_pre=None):
+    """Returns (r, h, rstd_post, rstd_pre), None where there is none: r without a block output and alpha 1 is x itself, h and its
+    rstd without a norm before the next block.  h has b's type (without b, x's)."""
+    device = _here(x, b, w_post, gate, w_pre, r, h, rstd_post, rstd_pre)
+    n, e = d.rows * d.cols, torch.empty
+    if r is None and not (b is None and d.alpha == 1.0): r = torch.empty_like(x)
+    if d.pre:
+        if h is None: h = torch.empty_like(x if b is None else b)
+        if rstd_pre is None: rstd_pre = e(d.rows, dtype=torch.float32, device=x.device)
+    if d.post and rstd_post is None: rstd_post = e(d.rows, dtype=torch.float32, device=x.device)
+    _check(lib.qbp_resnorm_fwd(C.addressof(d), _real(x, n, d.x_dtype, "x"), _real(b, n, d.b_dtype, "b"), _real(w_post, d.cols, QBP_F32, "w_post"),
+                               _real(gate, _gates(d) * d.cols, QBP_F32, "gate"), _real(w_pre, d.cols, QBP_F32, "w_pre"),
+                               _real(r, n, d.x_dtype, "r"), _real(h, n, d.b_dtype, "h"), _real(rstd_post, d.rows, QBP_F32, "rstd_post"),
+                               _real(rstd_pre, d.rows, QBP_F32, "rstd_pre"), _stream_handle(device)))
+    return r, h, rstd_post, rstd_pre
+
+
+def qbp_resnorm_bwd(d: ResnormDesc, dr, dh, b, r, rstd_post, rstd_pre, w_post=None, gate=None, w_pre=None, dx=None, db=None,
+                    want_params=True, ws=None):
+    """The gradients (dx, db, dw_post, dgate, dw_pre) from dr (None: nothing else uses r) and dh.  Gradients of what the forward
+    did not have are None; want_params=False: dx and db alone."""
+    device = _here(dr, dh, b, r, rstd_post, rstd_pre, w_post, gate, w_pre, dx, db, ws)
+    n, like = d.rows * d.cols, dr if dr is not None else r
+    if dx is None: dx = torch.empty_like(like)
+    if db is None and b is not None: db = torch.empty_like(b)
+    f32 = lambda *shape: torch.empty(shape, dtype=torch.float32, device=like.device)
+    dw1 = f32(d.cols) if want_params and d.post else None
+    dg = f32(_gates(d), d.cols) if want_params and gate is not None else None
+    dw2 = f32(d.cols) if want_params and d.pre else None
+    if ws is None: ws = workspace(lib.qbp_resnorm_bwd_workspace_bytes(C.addressof(d)), like.device)
+    _check(lib.qbp_resnorm_bwd(C.addressof(d), _real(dr, n, d.x_dtype, "dr"), _real(dh, n, d.b_dtype, "dh"), _real(b, n, d.b_dtype, "b"),
+                               _real(r, n, d.x_dtype, "r"), _real(rstd_post, d.rows, QBP_F32, "rstd_post"), _real(rstd_pre, d.rows, QBP_F32, "rstd_pre"),
+                               _real(w_post, d.cols, QBP_F32, "w_post"), _real(gate, _gates(d) * d.cols, QBP_F32, "gate"),
+                               _real(w_pre, d.cols, QBP_F32, "w_pre"), _real(dx, n, d.x_dtype, "dx"), _real(db, n, d.b_dtype, "db"),
+                               _addr(dw1), _addr(dg), _addr(dw2), ws.data_ptr(), ws.numel(), _stream_handle(device)))
+    return dx, db, dw1, dg, dw2
+
+
+def qbp_dropout(x, p, seed, tensor_id=0, index_base=0, y=None):
+    """y = x / (1 - p) where an element's draw keeps it, else 0 (p in steps of 2^-16).  The mask is made from (seed, tensor_id, the
+    element's index + index_base): the backward pass is the same call on the gradient."""
+    device = _here(x, y)
+    if y is None: y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    elif y.dtype != x.dtype or y.numel() != x.numel(): raise ValueError(f"y is {tuple(y.shape)} {y.dtype}, x {tuple(x.shape)} {x.dtype}")
+    _check(lib.qbp_dropout(_addr(x), _dtype(x.dtype), x.numel(), p, seed, tensor_id, index_base, _addr(y), _stream_handle(device)))
     return y
 
 
