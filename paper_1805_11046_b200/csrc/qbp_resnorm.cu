@@ -1,11 +1,20 @@
 // The join between two blocks of a residual network and its gradients (qbp_resnorm_fwd / _bwd in include/qbp.h): norm after a
 // block, gate, dropout, residual stream and the norm before the next block, in one pass over the rows.
 //
-// A row is held in registers by the threads of one group: a warp of a block's eight for rows of up to 1024 columns, the whole
-// block beyond; a thread has CH chunks of eight neighbouring columns.  The two sums over a row (of b^2 and of r^2; backwards of the
-// gradients' projections on r and b) each cost one exchange between the group's threads, and nothing is read twice.
-// Backwards a thread keeps the sums over its rows for its columns (dw_post, dgate, dw_pre) in registers, a block leaves one
-// partial row of each, and a second kernel adds these up in a fixed order.
+// A row is held in registers by the threads of one group: a warp (of a block's eight) for rows of up to 256 columns, a block of
+// up to 512 threads beyond; a thread has CH times eight columns.  The two sums over a row (of b^2 and of r^2; backwards of the
+// gradients' projections on r and b) are exchanged between the group's threads, forward a row's second with the next row's first, backwards
+// both at once, and nothing is read twice.  A block
+// takes neighbouring rows of one gate (an item) and keeps the parameters of its columns in registers.  Rows come through a ring of two
+// or three in shared memory that each thread fills and reads for itself (cp.async, no barrier): a row is on its way while the one before is worked on,
+// and stays out of the threads' registers.
+//
+// Backwards, with gate and w_post constant along an item's columns, dw_post and dgate are multiples of one sum over its rows,
+// S = sum of R dropout'(b rstd_post): dgate = w_post S, dw_post = gate S.  A thread keeps S and dw_pre's sum in registers, a block leaves
+// one partial row of each, and a second kernel adds these up in a fixed order.
+//
+// Columns.  Rows whose tensors all start on 16-byte boundaries are read eight neighbouring columns to a thread (VEC); others
+// with the lanes of a warp side by side, element by element, in a form for any type.
 #include "qbp_dropout.cuh"
 
 #include <algorithm>
@@ -15,268 +24,720 @@ namespace qbp {
 constexpr int kJoinWarpRows = 8;                    // rows of a block whose groups are warps
 constexpr int64_t kJoinMaxCols = QBP_RESNORM_MAX_COLS;
 
+// How the rows are cut: `gates` gates of `gate_rows` rows, each in `splits` items of `split_rows` rows (the last one fewer).
+struct JoinItems { int64_t rows, cols, gate_rows, gates, splits, split_rows; };
+
 struct JoinParams {
-    int64_t rows, cols, gate_rows;
+    JoinItems it;
     const void *x, *b; const float *w_post, *gate, *w_pre;
     void *r, *h; float *rstd_post, *rstd_pre;
     float eps, alpha, inv_cols;
-    int post, pre, drop, vec_x, vec_b, vec_w;
+    int post, pre, drop, x_dtype, b_dtype, wide;      // wide: outputs of fp32 start on 32-byte boundaries
     DropoutParams d;
 };
 
 struct JoinBwdParams {
-    int64_t rows, cols, gate_rows, gates, splits, split_rows;    // an item: `split_rows` rows of a gate (the last one fewer)
+    JoinItems it;
     const void *dr, *dh, *b, *r; const float *rstd_post, *rstd_pre, *w_post, *gate, *w_pre;
     void *dx, *db; float *part_post, *part_gate, *part_pre;
     float alpha, inv_cols;
-    int post, pre, drop, vec_x, vec_b, vec_w, sum_post, sum_gate, sum_pre;
+    int post, pre, drop, x_dtype, b_dtype, wide, sum_post, sum_gate, sum_pre;
     DropoutParams d;
 };
 
-// Sum over the threads of a row's group; every thread gets it.  WARP: the group is a warp.  `turn` alternates between the two
-// halves of the scratch, so that one barrier per sum is enough.
-template <bool WARP> __device__ __forceinline__ float group_sum(float v, float (&scratch)[2][32], int turn)
+#ifdef __CUDACC__
+// Eight elements of a row as a thread holds them.  VEC: neighbours, as they lie in memory; else 32 columns apart, as floats.
+struct AnyReal {};
+template <typename T> struct Held { Raw8<T> raw; };
+template <> struct Held<AnyReal> { float v[8]; };
+
+template <typename T> __device__ __forceinline__ void unpack8(const Held<T> &h, float (&v)[8]) { unpack8(h.raw, v); }
+__device__ __forceinline__ void unpack8(const Held<AnyReal> &h, float (&v)[8])
 {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    if (WARP) return v;
-    if ((threadIdx.x & 31) == 0) scratch[turn][threadIdx.x >> 5] = v;
-    __syncthreads();
-    float s = 0.0f;
-    for (unsigned w = 0; w < blockDim.x / 32; ++w) s += scratch[turn][w];
-    return s;
+    for (int e = 0; e < 8; ++e) v[e] = h.v[e];
 }
-
-// Eight fp32 parameters of neighbouring columns (absent: ones).
-__device__ __forceinline__ void load_params(const float *p, int64_t at, int n, int vec, float (&v)[8])
+// c: the thread's first column; columns at and behind `cols` are zero.
+template <typename T> __device__ __forceinline__ void load_row(Held<T> &h, const void *row0, int64_t base, int c, int cols, int)
+{
+    const T *p = static_cast<const T *>(row0) + base + c;
+    const bool in = c < cols;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) h.raw.w[i] = in ? reinterpret_cast<const uint4 *>(p)[i] : make_uint4(0, 0, 0, 0);   // (not __ldg: an output may lie over an input)
+}
+template <typename T> __device__ __forceinline__ void load_strided(float (&v)[8], const void *row0, int64_t base, int c, int cols)
+{
+    const T *p = static_cast<const T *>(row0) + base + c;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + 32 * e < cols ? real_of(p[32 * e]) : 0.0f;
+}
+__device__ __forceinline__ void load_row(Held<AnyReal> &h, const void *row0, int64_t base, int c, int cols, int dtype)
+{
+    QBP_FOR_DTYPE(dtype, T, load_strided<T>(h.v, row0, base, c, cols));
+}
+// Rounds to the type and stores; v is what the stored values stand for.
+template <typename T> __device__ __forceinline__ void store_row(const Held<T> &, void *row0, int64_t base, int c, int cols, int, float (&v)[8])
+{
+    const Raw8<T> r = pack8<T>(v);
+    T *p = static_cast<T *>(row0) + base + c;
+    if (row0 && c < cols) {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(T) / 2); ++i) reinterpret_cast<uint4 *>(p)[i] = r.w[i];
+    }
+    unpack8(r, v);
+}
+template <typename T> __device__ __forceinline__ void store_strided(void *row0, int64_t base, int c, int cols, float (&v)[8])
+{
+    T *p = static_cast<T *>(row0) + base + c;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const T t = real_to<T>(v[e]);
+        if (row0 && c + 32 * e < cols) p[32 * e] = t;
+        v[e] = real_of(t);
+    }
+}
+__device__ __forceinline__ void store_row(const Held<AnyReal> &, void *row0, int64_t base, int c, int cols, int dtype, float (&v)[8])
+{
+    QBP_FOR_DTYPE(dtype, T, store_strided<T>(row0, base, c, cols, v));
+}
+// fp32 parameters of the thread's columns (absent: ones; behind the last column anything).
+template <bool VEC> __device__ __forceinline__ void load_params(const float *p, int64_t base, int c, int cols, float (&v)[8])
 {
     if (!p) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = 1.0f;
+        for (int e = 0; e < 8; ++e) v[e] = 1.0f;
+    } else if (VEC) {
+        Held<float> h;
+        load_row(h, p, base, c, cols, QBP_F32);
+        unpack8(h, v);
     } else {
-        unpack8(load8(p + at, n, vec != 0), v);
+        load_strided<float>(v, p, base, c, cols);
     }
 }
-__device__ __forceinline__ void keep_factors(const DropoutParams &d, const PhiloxKeys &keys, int64_t element, float (&k8)[8])
-{
-    const uint4 w = dropout_draws8(d, keys, (uint64_t)element);
+// Which of a thread's eight elements a dropout keeps.  w0: the first of the warp's 256 columns, whose draws its lanes make eight
+// neighbours each; without VEC they then hand each other the results as bits.  drop: 1 by the draws, 2 none is kept.
+template <bool VEC> struct Kept {
+    uint4 w; uint32_t t;                             // VEC: the words, the threshold in the upper half; else the bits in w.x
+    __device__ __forceinline__ void make(const DropoutParams &d, const PhiloxKeys &keys, int drop, int64_t base, int w0)
+    {
+        const int lane = threadIdx.x & 31;
+        const uint64_t first = (uint64_t)(base + w0 + 8 * lane);
+        t = d.threshold << 16;
+        w = drop == 2 ? make_uint4(0u, 0u, 0u, 0u) : VEC ? dropout_block(d, keys, first >> 3) : dropout_draws8(d, keys, first);
+        if (drop == 2) t = 0xFFFF0000u;
+        if (VEC) return;
+        uint32_t bits = 0, mine = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) k8[k] = draw_of(w, k) >= d.threshold ? d.factor : 0.0f;
+        for (int e = 0; e < 8; ++e) bits |= (at_least(e) ? 1u : 0u) << e;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mine |= ((__shfl_sync(0xFFFFFFFFu, bits, 4 * e + (lane >> 3)) >> (lane & 7)) & 1u) << e;
+        w.x = mine;
+    }
+    // (the high half of a word against the threshold: the word itself against it in the upper half)
+    __device__ __forceinline__ bool at_least(int e) const
+    {
+        const uint32_t v = e < 2 ? w.x : e < 4 ? w.y : e < 6 ? w.z : w.w;
+        return ((e & 1) ? v : v << 16) >= t;
+    }
+    __device__ __forceinline__ bool operator[](int e) const { return VEC ? at_least(e) : ((w.x >> e) & 1u) != 0; }
+};
+
+// Sums over the threads of a row's group, N at a time; every thread gets them.  WARP: the group is a warp.  `turn` alternates between
+// the two halves of the scratch, so that one barrier an exchange is enough.
+constexpr int kJoinSums = 3;
+typedef float JoinScratch[2][kJoinSums][16];
+template <bool WARP, int N> __device__ __forceinline__ void group_sums(float (&v)[N], JoinScratch &scratch, int turn)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xFFFFFFFFu, v[n], o);
+    if (WARP) return;
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) scratch[turn][n][threadIdx.x >> 5] = v[n];
+    }
+    __syncthreads();
+    // (every warp adds up the warps' sums by itself: one load a lane and four exchanges)
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = (threadIdx.x & 15) < blockDim.x / 32 ? scratch[turn][n][threadIdx.x & 15] : 0.0f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xFFFFFFFFu, v[n], o);
+}
+template <bool WARP> __device__ __forceinline__ float group_sum(float v, JoinScratch &scratch, int turn)
+{
+    float a[1] = {v};
+    group_sums<WARP>(a, scratch, turn);
+    return a[0];
+}
+
+// The rows of an item: first, end.
+struct ItemRows { int64_t gate, first, end; };
+__device__ __forceinline__ ItemRows item_rows(const JoinItems &it, int64_t item)
+{
+    ItemRows r;
+    r.gate = item / it.splits;
+    r.first = r.gate * it.gate_rows + item % it.splits * it.split_rows;
+    r.end = min(min(r.first + it.split_rows, (r.gate + 1) * it.gate_rows), it.rows);
+    return r;
+}
+
+// A row's exchange of sums done, the next row's first one may write the half of the scratch that this row's last one is still read from,
+// where a row has one sum only.
+template <bool WARP> __device__ __forceinline__ void end_row(int pre, int post)
+{
+    if (!WARP && pre != post) __syncthreads();
+}
+
+// ---- rows read in vectors, through the ring ------------------------------------------------------------------------------
+// A thread's 16-byte pieces of a row lie side by side in its slot, an odd number of them (so that the slots of a quarter warp
+// fall into different banks), a slot for each of two turns.  Pieces behind the last column are cleared once and never written.
+template <typename T> struct Pieces { static constexpr int n = sizeof(T) / 2; };
+// The lanes of a warp copy 256 columns side by side, 16 bytes each at a time, into the slots of whoever reads them: of fp32 a lane's eight
+// columns are two such pieces, and copied by their reader each request would ask for half of 32 sectors.  slots: the first lane's; c: the
+// warp's first column.
+template <typename T, int SLOT> __device__ __forceinline__ void ring_fetch(uint4 *slots, const void *row0, int64_t at, int c, int cols)
+{
+    constexpr int n = Pieces<T>::n;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+        const int piece = 32 * i + (threadIdx.x & 31);
+        if (c + piece * (8 / n) < cols) cp_async16(slots + piece / n * SLOT + piece % n, static_cast<const T *>(row0) + at + piece * (8 / n));
+    }
+}
+template <typename T> __device__ __forceinline__ void ring_read(const uint4 *slot, float (&v)[8])
+{
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < Pieces<T>::n; ++i) r.w[i] = slot[i];
+    unpack8(r, v);
+}
+__device__ __forceinline__ void put32(void *p, const uint4 &a, const uint4 &b)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                 : "memory");
+}
+// (wide: fp32 rows start on 32-byte boundaries)
+template <typename T> __device__ __forceinline__ void put_vec(void *row0, int64_t at, const Raw8<T> &r, int wide)
+{
+    uint4 *p = reinterpret_cast<uint4 *>(static_cast<T *>(row0) + at);
+    if (Pieces<T>::n == 2 && wide) put32(p, r.w[0], r.w[Pieces<T>::n - 1]);
+    else {
+#pragma unroll
+        for (int i = 0; i < Pieces<T>::n; ++i) p[i] = r.w[i];
+    }
+}
+// gate * w_post of eight columns (zero behind the last one)
+__device__ __forceinline__ void join_gains(const float *gate, const float *w_post, int64_t gate_at, int c, bool in, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 1.0f;
+    if (!in) return;
+    if (gate) unpack8(load8(gate + gate_at + c, 8, true), v);
+    if (w_post) {
+        float w[8];
+        unpack8(load8(w_post + c, 8, true), w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= w[e];
+    }
 }
 
 template <typename TX, typename TB, int CH, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kJoinWarpRows : 512) join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ PhiloxKeys keys)
+__global__ void __launch_bounds__(WARP ? 32 * kJoinWarpRows : 512, WARP ? 2 : 1)
+join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ PhiloxKeys keys)
 {
-    __shared__ float scratch[2][32];
-    const int group = WARP ? 32 : blockDim.x, t = WARP ? (threadIdx.x & 31) : threadIdx.x;
-    const int64_t step = WARP ? (int64_t)gridDim.x * kJoinWarpRows : gridDim.x;
-    pdl_wait();
-    for (int64_t row = WARP ? (int64_t)blockIdx.x * kJoinWarpRows + (threadIdx.x >> 5) : blockIdx.x; row < P.rows; row += step) {
-        const int64_t base = row * P.cols, grow = P.gate_rows ? row / P.gate_rows : 0;
-        Raw8<TX> xr[CH]; Raw8<TB> br[CH];
-        int n[CH];
+    extern __shared__ uint4 ring[];
+    __shared__ JoinScratch scratch;
+    constexpr int px = Pieces<TX>::n, pb = Pieces<TB>::n, kSlot = (CH * (px + pb)) | 1;
+    const int lane = threadIdx.x & 31, warp = WARP ? 0 : threadIdx.x >> 5, warps = WARP ? 1 : blockDim.x >> 5;
+    const int sub = WARP ? threadIdx.x >> 5 : 0, subs = WARP ? kJoinWarpRows : 1;
+    const int cols = (int)P.it.cols, c0 = 256 * warp + 8 * lane, apart = 256 * warps;      // the thread's first column, and its next ones'
+    const int turn_units = blockDim.x * kSlot;
+    uint4 *const mine = ring + threadIdx.x * kSlot;
+    bool in[CH];
+    float gw[CH][8], w2[CH][8];
 #pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            const int64_t c = 8ll * (t + k * group);
-            n[k] = (int)max((int64_t)0, min((int64_t)8, P.cols - c));
-            xr[k] = load8(static_cast<const TX *>(P.x) + (n[k] ? base + c : 0), n[k], P.vec_x != 0);
-            if (P.b) br[k] = load8(static_cast<const TB *>(P.b) + (n[k] ? base + c : 0), n[k], P.vec_b != 0);
-        }
-        float rstd = 1.0f;
-        if (P.post) {
-            float s = 0.0f;
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                float v[8];
-                unpack8(br[k], v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
-            }
-            rstd = 1.0f / sqrtf(group_sum<WARP>(s, scratch, 0) * P.inv_cols + P.eps);
-            if (P.rstd_post && t == 0) P.rstd_post[row] = rstd;
-        }
-        float s2 = 0.0f;
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            const int64_t c = 8ll * (t + k * group);
-            float x[8];
-            unpack8(xr[k], x);
-            if (P.b) {
-                float b[8], w[8], g[8], m[8];
-                unpack8(br[k], b);
-                load_params(P.post ? P.w_post : nullptr, c, n[k], P.vec_w, w);
-                load_params(P.gate, grow * P.cols + c, n[k], P.vec_w, g);
-                if (P.drop) keep_factors(P.d, keys, base + c, m);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float v = P.post ? b[e] * rstd * w[e] : b[e];
-                    if (P.drop) v = m[e] != 0.0f ? v * m[e] : 0.0f;
-                    x[e] = P.alpha * x[e] + g[e] * v;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = P.alpha * x[e];
-            }
-            xr[k] = pack8<TX>(x);
-            if (P.r && n[k]) store8(static_cast<TX *>(P.r) + base + c, xr[k], n[k], P.vec_x != 0);
-            unpack8(xr[k], x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s2 = e < n[k] ? fmaf(x[e], x[e], s2) : s2;
-        }
-        if (P.pre) {
-            const float rstd2 = 1.0f / sqrtf(group_sum<WARP>(s2, scratch, 1) * P.inv_cols + P.eps);
-            if (P.rstd_pre && t == 0) P.rstd_pre[row] = rstd2;
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                const int64_t c = 8ll * (t + k * group);
-                float x[8], w[8];
-                unpack8(xr[k], x);
-                load_params(P.w_pre, c, n[k], P.vec_w, w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = x[e] * rstd2 * w[e];
-                if (n[k]) store8(static_cast<TB *>(P.h) + base + c, pack8<TB>(x), n[k], P.vec_b != 0);
-            }
-        }
-        if (!WARP && P.pre != P.post) __syncthreads();   // one sum a row: the next row's writes the half that this one's may still be read from
+    for (int k = 0; k < CH; ++k) {
+        in[k] = c0 + k * apart < cols;
+        for (int i = 0; i < px + pb; ++i)
+            if (!in[k] || (!P.b && i >= px))
+                for (int t = 0; t < 3; ++t) mine[t * turn_units + k * (px + pb) + i] = make_uint4(0, 0, 0, 0);
     }
-}
-
-template <typename TX, typename TB, int CH, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kJoinWarpRows : 512) join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__ PhiloxKeys keys)
-{
-    extern __shared__ float fold[];                  // WARP: [kJoinWarpRows][cols rounded up to 8], the warps' sums
-    __shared__ float scratch[2][32];
-    const int group = WARP ? 32 : blockDim.x, t = WARP ? (threadIdx.x & 31) : threadIdx.x, sub = WARP ? threadIdx.x >> 5 : 0;
-    const int subs = WARP ? kJoinWarpRows : 1;
-    const int64_t pitch = (P.cols + 7) / 8 * 8;
-    float a_post[CH][8] = {}, a_gate[CH][8] = {}, a_pre[CH][8] = {};
-    // A thread's sums of one kind to the block's partial row (and back to zero).
-    const auto leave = [&](float (&a)[CH][8], float *out) {
-        if (WARP) {
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                const int64_t c = 8ll * (t + k * group);
-                if (c < P.cols) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) fold[sub * pitch + c + e] = a[k][e];
-                }
-            }
-            __syncthreads();
-            for (int64_t c = threadIdx.x; c < P.cols; c += blockDim.x) {
-                float s = 0.0f;
-#pragma unroll
-                for (int q = 0; q < kJoinWarpRows; ++q) s += fold[q * pitch + c];
-                out[c] = s;
-            }
-        } else {
-#pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                const int64_t c = 8ll * (t + k * group);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (c + e < P.cols) out[c + e] = a[k][e];
-            }
-        }
+    const auto fetch = [&](int64_t row, int64_t end, uint4 *slot) {
+        const int c = 256 * warp;
+        const int64_t at = row * cols + c;
+        slot -= lane * kSlot;
+        __syncwarp();                                  // (every lane has read what the slots held)
 #pragma unroll
         for (int k = 0; k < CH; ++k)
+            if (row < end) {
+                ring_fetch<TX, kSlot>(slot + k * (px + pb), P.x, at + k * apart, c + k * apart, cols);
+                if (P.b) ring_fetch<TB, kSlot>(slot + k * (px + pb) + px, P.b, at + k * apart, c + k * apart, cols);
+            }
+        cp_async_commit();
+    };
+    const auto square_sum = [&](const uint4 *slot) {
+        float s = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[k][e] = 0.0f;
+        for (int k = 0; k < CH; ++k) {
+            float v[8];
+            ring_read<TB>(slot + k * (px + pb) + px, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
+        }
+        return s;
     };
     pdl_wait();
-    for (int64_t item = blockIdx.x; item < P.gates * P.splits; item += gridDim.x) {
-        const int64_t g = item / P.splits, first = g * P.gate_rows + item % P.splits * P.split_rows;
-        const int64_t end = min(min(first + P.split_rows, (g + 1) * P.gate_rows), P.rows);
-        for (int64_t row = first + sub; row < end; row += subs) {
-            const int64_t base = row * P.cols;
-            Raw8<TX> gr[CH], rr[CH]; Raw8<TB> hr[CH], br[CH];
-            int n[CH];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) join_gains(P.w_pre, nullptr, 0, c0 + k * apart, in[k], w2[k]);
+    const float factor = P.drop ? P.d.factor : 1.0f;
+    int64_t had = -1;
+    int half = 0;
+    for (int64_t item = blockIdx.x; item < P.it.gates * P.it.splits; item += gridDim.x) {
+        const ItemRows rows = item_rows(P.it, item);
+        uint4 *slot = mine, *slot1 = mine + turn_units, *slot2 = mine + 2 * turn_units;
+        fetch(rows.first + sub, rows.end, slot);
+        fetch(rows.first + sub + subs, rows.end, slot1);
+        if (P.b && rows.gate != had) {
+#pragma unroll
+            for (int k = 0; k < CH; ++k) join_gains(P.gate, P.post ? P.w_post : nullptr, rows.gate * cols, c0 + k * apart, in[k], gw[k]);
+            had = rows.gate;
+        }
+        cp_async_wait<1>();
+        __syncwarp();
+        float rstd = 1.0f;
+        if (P.post) { rstd = rsqrtf(group_sum<WARP>(square_sum(slot), scratch, half) * P.inv_cols + P.eps); half ^= 1; }
+        for (int64_t row = rows.first + sub; row < rows.end; row += subs) {
+            fetch(row + 2 * subs, rows.end, slot2);
+            const int64_t at = row * cols + c0;
+            if (P.post && P.rstd_post && warp == 0 && lane == 0) P.rstd_post[row] = rstd;
+            const float scale = factor * rstd;
+            float r[CH][8], sums[2] = {0.0f, 0.0f};           // of this row's r^2, of the next row's b^2
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
-                const int64_t c = 8ll * (t + k * group);
-                n[k] = (int)max((int64_t)0, min((int64_t)8, P.cols - c));
-                const int64_t at = n[k] ? base + c : 0;
-                gr[k] = load8(static_cast<const TX *>(P.dr) + (P.dr ? at : 0), P.dr ? n[k] : 0, P.vec_x != 0);
-                if (P.pre) { rr[k] = load8(static_cast<const TX *>(P.r) + at, n[k], P.vec_x != 0); hr[k] = load8(static_cast<const TB *>(P.dh) + at, n[k], P.vec_b != 0); }
-                if (P.b) br[k] = load8(static_cast<const TB *>(P.b) + at, n[k], P.vec_b != 0);
+                ring_read<TX>(slot + k * (px + pb), r[k]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) r[k][e] *= P.alpha;
+                if (P.b) {
+                    float b[8];
+                    ring_read<TB>(slot + k * (px + pb) + px, b);
+                    if (P.drop) {                     // (what is dropped counts for nothing, whatever it is: chosen, not multiplied by zero)
+                        Kept<true> kept;
+                        kept.make(P.d, keys, P.drop, at - 8 * lane + k * apart, 0);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) b[e] = kept[e] ? b[e] : 0.0f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) r[k][e] = fmaf(b[e] * scale, gw[k][e], r[k][e]);
+                }
+                const Raw8<TX> raw = pack8<TX>(r[k]);
+                if (P.r && in[k]) put_vec(P.r, at + k * apart, raw, P.wide);
+                unpack8(raw, r[k]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sums[0] = fmaf(r[k][e], r[k][e], sums[0]);    // (zero behind the last column, as x and b are)
             }
-            float rstd2 = 0.0f, mean2 = 0.0f;
+            cp_async_wait<1>();
+            __syncwarp();
+            if (P.post) sums[1] = square_sum(slot1);
+            group_sums<WARP>(sums, scratch, half);
+            half ^= 1;
+            rstd = P.post ? rsqrtf(sums[1] * P.inv_cols + P.eps) : 1.0f;
             if (P.pre) {
-                rstd2 = P.rstd_pre[row];
+                const float rstd2 = rsqrtf(sums[0] * P.inv_cols + P.eps);
+                if (P.rstd_pre && warp == 0 && lane == 0) P.rstd_pre[row] = rstd2;
+#pragma unroll
+                for (int k = 0; k < CH; ++k) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) r[k][e] = r[k][e] * rstd2 * w2[k][e];
+                    if (in[k]) put_vec(P.h, at + k * apart, pack8<TB>(r[k]), P.wide);
+                }
+            }
+            uint4 *const t = slot; slot = slot1; slot1 = slot2; slot2 = t;
+        }
+        cp_async_wait<0>();
+    }
+}
+
+// A thread's sums of one kind over an item's rows to the block's partial row, times parameters of its columns (nullable).  added: to
+// what an item before of this block left there.  VEC: eight neighbouring columns, else 32 apart.
+template <int CH, bool WARP, bool VEC>
+__device__ __forceinline__ void join_leave(const float (&a)[CH][8], float *out, const float *w, int cols, int c0, int apart, bool added, float *fold)
+{
+    if (WARP) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        float m[8];
+        load_params<VEC>(w, 0, c0 + k * apart, cols, m);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = c0 + k * apart + (VEC ? e : 32 * e);
+            const float v = a[k][e] * m[e];
+            if (WARP) fold[(threadIdx.x >> 5) * 256 * CH + c] = v;
+            else if (c < cols) out[c] = added ? out[c] + v : v;
+        }
+    }
+    if (WARP) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+            float s = added ? out[c] : 0.0f;
+#pragma unroll
+            for (int q = 0; q < kJoinWarpRows; ++q) s += fold[q * 256 * CH + c];
+            out[c] = s;
+        }
+    }
+}
+
+template <typename TX, typename TB, int CH, bool WARP>
+__global__ void __launch_bounds__(WARP ? 32 * kJoinWarpRows : 512, 1)
+join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__ PhiloxKeys keys)
+{
+    extern __shared__ uint4 ring[];
+    __shared__ float fold[WARP ? kJoinWarpRows * 256 * CH : 1];            // WARP: the warps' sums
+    __shared__ JoinScratch scratch;
+    // pieces of dr, r, dh, b
+    constexpr int px = Pieces<TX>::n, pb = Pieces<TB>::n, at_r = px, at_h = 2 * px, at_b = 2 * px + pb, row_units = 2 * (px + pb), kSlot = (CH * row_units) | 1;
+    const int lane = threadIdx.x & 31, warp = WARP ? 0 : threadIdx.x >> 5, warps = WARP ? 1 : blockDim.x >> 5;
+    const int sub = WARP ? threadIdx.x >> 5 : 0, subs = WARP ? kJoinWarpRows : 1;
+    const int cols = (int)P.it.cols, c0 = 256 * warp + 8 * lane, apart = 256 * warps;
+    const int turn_units = blockDim.x * kSlot;
+    uint4 *const mine = ring + threadIdx.x * kSlot;
+    bool in[CH];
+    float gw[CH][8], w2[CH][8], a_pre[CH][8] = {};
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        in[k] = c0 + k * apart < cols;
+        for (int i = 0; i < row_units; ++i)
+            if (!in[k] || (!P.dr && i < at_r) || (!P.pre && i >= at_r && i < at_b) || (!P.b && i >= at_b))
+                mine[k * row_units + i] = mine[turn_units + k * row_units + i] = make_uint4(0, 0, 0, 0);
+    }
+    const auto fetch = [&](int64_t row, int turn) {
+        const int c = 256 * warp;
+        uint4 *slot = mine - lane * kSlot + turn * turn_units;
+        const int64_t at = row * cols + c;
+        __syncwarp();                                  // (every lane has read what the slots held)
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            if (P.dr) ring_fetch<TX, kSlot>(slot + k * row_units, P.dr, at + k * apart, c + k * apart, cols);
+            if (P.pre) {
+                ring_fetch<TX, kSlot>(slot + k * row_units + at_r, P.r, at + k * apart, c + k * apart, cols);
+                ring_fetch<TB, kSlot>(slot + k * row_units + at_h, P.dh, at + k * apart, c + k * apart, cols);
+            }
+            if (P.b) ring_fetch<TB, kSlot>(slot + k * row_units + at_b, P.b, at + k * apart, c + k * apart, cols);
+        }
+        cp_async_commit();
+    };
+    pdl_wait();
+#pragma unroll
+    for (int k = 0; k < CH; ++k) join_gains(P.w_pre, nullptr, 0, c0 + k * apart, in[k], w2[k]);
+    const float factor = P.drop ? P.d.factor : 1.0f;
+    int half = 0;
+    for (int64_t item = blockIdx.x; item < P.it.gates * P.it.splits; item += gridDim.x) {
+        const ItemRows rows = item_rows(P.it, item);
+        float S[CH][8] = {};                          // of R dropout' b rstd_post
+        int turn = 0;
+        if (rows.first + sub < rows.end) fetch(rows.first + sub, 0);
+#pragma unroll
+        for (int k = 0; k < CH; ++k) join_gains(P.gate, P.post ? P.w_post : nullptr, rows.gate * cols, c0 + k * apart, in[k], gw[k]);
+        for (int64_t row = rows.first + sub; row < rows.end; row += subs, turn ^= 1) {
+            const uint4 *slot = mine + turn * turn_units;
+            const float rstd1 = P.post ? __ldg(P.rstd_post + row) : 1.0f, rstd2 = P.pre ? __ldg(P.rstd_pre + row) : 0.0f;
+            if (row + subs < rows.end) { fetch(row + subs, turn ^ 1); cp_async_wait<1>(); }
+            else cp_async_wait<0>();
+            __syncwarp();
+            const int64_t at = row * cols + c0;
+            // Both means from one exchange: the second, of v w_post b, is linear in the first, m, with R = (dr + dh w_pre rstd_pre) - r m.
+            float sums[3] = {0.0f, 0.0f, 0.0f};
+            uint32_t kept = 0;                        // which elements the dropout keeps, a bit each
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                float h[8], r[8], g[8], b[8];
+                ring_read<TB>(slot + k * row_units + at_h, h);
+                ring_read<TX>(slot + k * row_units + at_r, r);
+                ring_read<TX>(slot + k * row_units, g);
+                ring_read<TB>(slot + k * row_units + at_b, b);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    a_pre[k][e] = fmaf(h[e] * r[e], rstd2, a_pre[k][e]);
+                    h[e] *= w2[k][e];
+                    sums[0] = fmaf(h[e], r[e], sums[0]);
+                    b[e] *= gw[k][e];
+                }
+                if (P.drop) {
+                    Kept<true> q;
+                    q.make(P.d, keys, P.drop, at - 8 * lane + k * apart, 0);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { const bool on = q[e]; kept |= on ? 1u << (8 * k + e) : 0u; b[e] = on ? b[e] : 0.0f; }
+                }
+                if (P.post) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        sums[1] = fmaf(fmaf(h[e], rstd2, g[e]), b[e], sums[1]);
+                        sums[2] = fmaf(r[e], b[e], sums[2]);
+                    }
+                }
+            }
+            if (P.pre || P.post) { group_sums<WARP>(sums, scratch, half); half ^= 1; }
+            // R = dr + rstd2 (dh w_pre) - r m2;  db = z rstd1 - b m1 with z = R dropout' gate w_post
+            const float m2 = P.pre ? sums[0] * P.inv_cols * rstd2 * rstd2 * rstd2 : 0.0f;
+            const float m1 = P.post ? (sums[1] - m2 * sums[2]) * factor * P.inv_cols * rstd1 * rstd1 * rstd1 : 0.0f;
+            const float f1 = factor * rstd1;
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                float R[8];
+                ring_read<TX>(slot + k * row_units, R);
+                if (P.pre) {
+                    float h[8], r[8];
+                    ring_read<TB>(slot + k * row_units + at_h, h);
+                    ring_read<TX>(slot + k * row_units + at_r, r);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) R[e] = fmaf(-r[e], m2, fmaf(h[e] * w2[k][e], rstd2, R[e]));
+                }
+                if (P.b) {
+                    float b[8], z[8];
+                    ring_read<TB>(slot + k * row_units + at_b, b);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = R[e] * f1;
+                    if (P.drop) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const bool on = (kept >> (8 * k + e)) & 1u;
+                            z[e] = on ? z[e] : 0.0f;
+                            S[k][e] = on ? fmaf(z[e], b[e], S[k][e]) : S[k][e];
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) S[k][e] = fmaf(z[e], b[e], S[k][e]);
+                    }
+                    if (P.db && in[k]) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] = P.post ? fmaf(-b[e], m1, z[e] * gw[k][e]) : z[e] * gw[k][e];
+                        put_vec(P.db, at + k * apart, pack8<TB>(z), P.wide);
+                    }
+                }
+                if (P.dx && in[k]) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) R[e] *= P.alpha;
+                    put_vec(P.dx, at + k * apart, pack8<TX>(R), P.wide);
+                }
+            }
+        }
+        if (P.sum_gate) join_leave<CH, WARP, true>(S, P.part_gate + item * cols, P.post ? P.w_post : nullptr, cols, c0, apart, false, fold);
+        if (P.sum_post) join_leave<CH, WARP, true>(S, P.part_post + (int64_t)blockIdx.x * cols, P.gate ? P.gate + rows.gate * cols : nullptr, cols, c0, apart, item != blockIdx.x, fold);
+    }
+    if (P.sum_pre) join_leave<CH, WARP, true>(a_pre, P.part_pre + (int64_t)blockIdx.x * cols, nullptr, cols, c0, apart, false, fold);
+}
+
+// ---- any rows -------------------------------------------------------------------------------------------------------------
+template <typename TX, typename TB, int CH> struct JoinRow { Held<TX> x[CH]; Held<TB> b[CH]; };
+
+template <typename TX, typename TB, int CH, bool WARP, bool VEC>
+__global__ void __launch_bounds__(WARP ? 32 * kJoinWarpRows : 512, 1)
+join_fwd_any_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ PhiloxKeys keys)
+{
+    __shared__ JoinScratch scratch;
+    const int lane = threadIdx.x & 31, warp = WARP ? 0 : threadIdx.x >> 5, warps = WARP ? 1 : blockDim.x >> 5;
+    const int sub = WARP ? threadIdx.x >> 5 : 0, subs = WARP ? kJoinWarpRows : 1;
+    const int cols = (int)P.it.cols;
+    const auto w0 = [&](int k) { return 256 * (warp + k * warps); };
+    const auto col = [&](int k) { return w0(k) + (VEC ? 8 * lane : lane); };
+    const auto fetch = [&](JoinRow<TX, TB, CH> &R, int64_t row) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            load_row(R.x[k], P.x, row * (int64_t)cols, col(k), cols, P.x_dtype);
+            if (P.b) load_row(R.b[k], P.b, row * (int64_t)cols, col(k), cols, P.b_dtype);
+        }
+    };
+    pdl_wait();
+    for (int64_t item = blockIdx.x; item < P.it.gates * P.it.splits; item += gridDim.x) {
+        const ItemRows rows = item_rows(P.it, item);
+        JoinRow<TX, TB, CH> R;
+        for (int64_t row = rows.first + sub; row < rows.end; row += subs) {
+            fetch(R, row);
+            const int64_t base = row * (int64_t)cols;
+            const auto get_x = [&](int k, float (&v)[8]) { unpack8(R.x[k], v); };
+            const auto get_b = [&](int k, float (&v)[8]) { unpack8(R.b[k], v); };
+            float rstd = 1.0f;
+            if (P.post) {
+                float s = 0.0f;
+#pragma unroll
+                for (int k = 0; k < CH; ++k) {
+                    float v[8];
+                    get_b(k, v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
+                }
+                rstd = rsqrtf(group_sum<WARP>(s, scratch, 0) * P.inv_cols + P.eps);
+                if (P.rstd_post && warp == 0 && lane == 0) P.rstd_post[row] = rstd;
+            }
+            float s2 = 0.0f, r8[CH][8];
+#pragma unroll
+            for (int k = 0; k < CH; ++k) {
+                get_x(k, r8[k]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) r8[k][e] *= P.alpha;
+                if (P.b) {
+                    float b[8], w[8];
+                    get_b(k, b);
+                    const float scale = P.drop ? rstd * P.d.factor : rstd;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) b[e] *= scale;
+                    if (P.post && P.w_post) {
+                        load_params<VEC>(P.w_post, 0, col(k), cols, w);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) b[e] *= w[e];
+                    }
+                    load_params<VEC>(P.gate, rows.gate * (int64_t)cols, col(k), cols, w);
+                    Kept<VEC> kept;
+                    if (P.drop) kept.make(P.d, keys, P.drop, base, w0(k));
+                    // (what is dropped counts for nothing, whatever it is: chosen, not multiplied by zero)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) b[e] = !P.drop || kept[e] ? b[e] : 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) r8[k][e] = fmaf(b[e], w[e], r8[k][e]);
+                }
+                store_row(R.x[k], P.r, base, col(k), cols, P.x_dtype, r8[k]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s2 = fmaf(r8[k][e], r8[k][e], s2);      // (zero behind the last column, as x and b are)
+            }
+            if (P.pre) {
+                const float rstd2 = rsqrtf(group_sum<WARP>(s2, scratch, 1) * P.inv_cols + P.eps);
+                if (P.rstd_pre && warp == 0 && lane == 0) P.rstd_pre[row] = rstd2;
+#pragma unroll
+                for (int k = 0; k < CH; ++k) {
+                    float w[8];
+                    load_params<VEC>(P.w_pre, 0, col(k), cols, w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) r8[k][e] = r8[k][e] * rstd2 * w[e];
+                    store_row(R.b[k], P.h, base, col(k), cols, P.b_dtype, r8[k]);
+                }
+            }
+            end_row<WARP>(P.pre, P.post);
+        }
+    }
+}
+
+template <typename TX, typename TB, int CH> struct JoinBwdRow { Held<TX> g[CH], r[CH]; Held<TB> h[CH], b[CH]; };
+
+template <typename TX, typename TB, int CH, bool WARP, bool VEC>
+__global__ void __launch_bounds__(WARP ? 32 * kJoinWarpRows : 512, 1)
+join_bwd_any_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__ PhiloxKeys keys)
+{
+    __shared__ float fold[WARP ? kJoinWarpRows * 256 * CH : 1];
+    __shared__ JoinScratch scratch;
+    const int lane = threadIdx.x & 31, warp = WARP ? 0 : threadIdx.x >> 5, warps = WARP ? 1 : blockDim.x >> 5;
+    const int sub = WARP ? threadIdx.x >> 5 : 0, subs = WARP ? kJoinWarpRows : 1;
+    const int cols = (int)P.it.cols;
+    const auto w0 = [&](int k) { return 256 * (warp + k * warps); };
+    const auto col = [&](int k) { return w0(k) + (VEC ? 8 * lane : lane); };
+    const auto fetch = [&](JoinBwdRow<TX, TB, CH> &R, int64_t row) {
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            if (P.dr) load_row(R.g[k], P.dr, row * (int64_t)cols, col(k), cols, P.x_dtype);
+            if (P.pre) { load_row(R.r[k], P.r, row * (int64_t)cols, col(k), cols, P.x_dtype); load_row(R.h[k], P.dh, row * (int64_t)cols, col(k), cols, P.b_dtype); }
+            if (P.b) load_row(R.b[k], P.b, row * (int64_t)cols, col(k), cols, P.b_dtype);
+        }
+    };
+    float a_pre[CH][8] = {};
+    pdl_wait();
+    for (int64_t item = blockIdx.x; item < P.it.gates * P.it.splits; item += gridDim.x) {
+        const ItemRows rows = item_rows(P.it, item);
+        float S[CH][8] = {};
+        JoinBwdRow<TX, TB, CH> R;
+        for (int64_t row = rows.first + sub; row < rows.end; row += subs) {
+            fetch(R, row);
+            const int64_t base = row * (int64_t)cols;
+            const float rstd1 = P.post ? __ldg(P.rstd_post + row) : 1.0f, rstd2 = P.pre ? __ldg(P.rstd_pre + row) : 0.0f;
+            const auto get_g = [&](int k, float (&v)[8]) { unpack8(R.g[k], v); };
+            const auto get_r = [&](int k, float (&v)[8]) { unpack8(R.r[k], v); };
+            const auto get_h = [&](int k, float (&v)[8]) { unpack8(R.h[k], v); };
+            const auto get_b = [&](int k, float (&v)[8]) { unpack8(R.b[k], v); };
+            float mean2 = 0.0f;
+            if (P.pre) {
                 float s = 0.0f;
 #pragma unroll
                 for (int k = 0; k < CH; ++k) {
                     float h[8], r[8], w[8];
-                    unpack8(hr[k], h); unpack8(rr[k], r);
-                    load_params(P.w_pre, 8ll * (t + k * group), n[k], P.vec_w, w);
+                    get_h(k, h); get_r(k, r);
+                    load_params<VEC>(P.w_pre, 0, col(k), cols, w);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float rh = r[e] * rstd2;
-                        a_pre[k][e] = fmaf(h[e], rh, a_pre[k][e]);
-                        s = fmaf(h[e] * w[e], rh, s);
+                        const float t = h[e] * (r[e] * rstd2);
+                        a_pre[k][e] += t;
+                        s = fmaf(t, w[e], s);
                     }
                 }
                 mean2 = group_sum<WARP>(s, scratch, 0) * P.inv_cols;
             }
-            const float rstd1 = P.post ? P.rstd_post[row] : 1.0f;
-            float s1 = 0.0f;
-            float v8[CH][8];                             // v w_post of the row (without a post norm: v)
+            float s1 = 0.0f, z[CH][8];                   // z = R dropout' gate w_post
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
-                const int64_t c = 8ll * (t + k * group);
-                float R[8];
-                unpack8(gr[k], R);
+                float g[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] = 0.0f;
+                if (P.dr) get_g(k, g);
                 if (P.pre) {
                     float h[8], r[8], w[8];
-                    unpack8(hr[k], h); unpack8(rr[k], r);
-                    load_params(P.w_pre, c, n[k], P.vec_w, w);
+                    get_h(k, h); get_r(k, r);
+                    load_params<VEC>(P.w_pre, 0, col(k), cols, w);
+                    const float m = mean2 * rstd2;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) R[e] += rstd2 * (h[e] * w[e] - r[e] * rstd2 * mean2);
+                    for (int e = 0; e < 8; ++e) g[e] = fmaf(rstd2, h[e] * w[e] - r[e] * m, g[e]);
                 }
                 if (P.b) {
-                    float b[8], w[8], gt[8], m[8];
-                    unpack8(br[k], b);
-                    load_params(P.post ? P.w_post : nullptr, c, n[k], P.vec_w, w);
-                    load_params(P.gate, g * P.cols + c, n[k], P.vec_w, gt);
-                    if (P.drop) keep_factors(P.d, keys, base + c, m);
+                    float b[8], w[8];
+                    get_b(k, b);
+                    Kept<VEC> kept;
+                    if (P.drop) kept.make(P.d, keys, P.drop, base, w0(k));
+                    const float f = P.drop ? P.d.factor : 1.0f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const float bh = b[e] * rstd1, q = P.drop ? m[e] : 1.0f;
-                        const float v = q != 0.0f ? R[e] * gt[e] * q : 0.0f;
-                        a_gate[k][e] += q != 0.0f ? R[e] * (bh * w[e] * q) : 0.0f;
-                        a_post[k][e] = fmaf(v, bh, a_post[k][e]);
-                        v8[k][e] = v * w[e];
-                        s1 = fmaf(v8[k][e], bh, s1);
+                        const bool keep = !P.drop || kept[e];
+                        z[k][e] = keep ? g[e] * f : 0.0f;
+                        b[e] *= rstd1;
+                        S[k][e] = fmaf(z[k][e], keep ? b[e] : 0.0f, S[k][e]);
+                    }
+                    load_params<VEC>(P.gate, rows.gate * (int64_t)cols, col(k), cols, w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[k][e] *= w[e];
+                    if (P.post) {
+                        load_params<VEC>(P.w_post, 0, col(k), cols, w);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) { z[k][e] *= w[e]; s1 = fmaf(z[k][e], b[e], s1); }
                     }
                 }
-                if (P.dx && n[k]) {
+                if (P.dx) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) R[e] *= P.alpha;
-                    store8(static_cast<TX *>(P.dx) + base + c, pack8<TX>(R), n[k], P.vec_x != 0);
+                    for (int e = 0; e < 8; ++e) g[e] *= P.alpha;
+                    store_row(R.g[k], P.dx, base, col(k), cols, P.x_dtype, g);
                 }
             }
             if (P.b) {
-                const float mean1 = P.post ? group_sum<WARP>(s1, scratch, 1) * P.inv_cols : 0.0f;
+                const float mean1 = P.post ? group_sum<WARP>(s1, scratch, 1) * P.inv_cols * rstd1 : 0.0f;
                 if (P.db) {
 #pragma unroll
                     for (int k = 0; k < CH; ++k) {
                         if (P.post) {
                             float b[8];
-                            unpack8(br[k], b);
+                            get_b(k, b);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v8[k][e] = rstd1 * (v8[k][e] - b[e] * rstd1 * mean1);
+                            for (int e = 0; e < 8; ++e) z[k][e] = rstd1 * (z[k][e] - b[e] * mean1);
                         }
-                        if (n[k]) store8(static_cast<TB *>(P.db) + base + 8ll * (t + k * group), pack8<TB>(v8[k]), n[k], P.vec_b != 0);
+                        store_row(R.b[k], P.db, base, col(k), cols, P.b_dtype, z[k]);
                     }
                 }
             }
-            if (!WARP && P.pre != P.post) __syncthreads();   // one sum a row: the next row's writes the half that this one's may still be read from
+            end_row<WARP>(P.pre, P.post);
         }
-        if (P.sum_gate) leave(a_gate, P.part_gate + item * P.cols);
+        if (P.sum_gate) join_leave<CH, WARP, VEC>(S, P.part_gate + item * (int64_t)cols, P.post ? P.w_post : nullptr, cols, col(0), 256 * warps, false, fold);
+        if (P.sum_post)
+            join_leave<CH, WARP, VEC>(S, P.part_post + (int64_t)blockIdx.x * cols, P.gate ? P.gate + rows.gate * (int64_t)cols : nullptr, cols, col(0), 256 * warps,
+                                      item != blockIdx.x, fold);
     }
-    if (P.sum_post) leave(a_post, P.part_post + (int64_t)blockIdx.x * P.cols);
-    if (P.sum_pre) leave(a_pre, P.part_pre + (int64_t)blockIdx.x * P.cols);
+    if (P.sum_pre) join_leave<CH, WARP, VEC>(a_pre, P.part_pre + (int64_t)blockIdx.x * cols, nullptr, cols, col(0), 256 * warps, false, fold);
 }
+#endif
 
 // out[o][c] = sum over `count` partial rows in [outs][count][cols], in a fixed order: sixteen threads of a column take every sixteenth, then
 // the sixteen are added up.
@@ -311,31 +772,43 @@ __global__ void __launch_bounds__(32 * kSumHigh) join_sum_kernel(const __grid_co
 
 // ================================================================= host side
 struct JoinShape { int ch, threads; bool warp; };
-static JoinShape join_shape(int64_t cols)
+constexpr size_t kJoinMaxRing = 200 * 1024, kJoinSmRings = 222 * 1024;        // of a block, of an SM
+// Shared memory of a block's ring: three rows forward, with one tensor of each type, and two backwards, with two.
+static size_t join_ring(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
 {
-    const int64_t chunks = (cols + 7) / 8;
-    if (chunks <= 32) return {1, 32 * kJoinWarpRows, true};
-    if (chunks <= 64) return {2, 32 * kJoinWarpRows, true};
-    if (chunks <= 128) return {4, 32 * kJoinWarpRows, true};
-    if (chunks <= 256) return {2, 128, false};
-    if (chunks <= 512) return {2, 256, false};
-    if (chunks <= 1024) return {2, 512, false};
-    return {4, 512, false};
+    const size_t pieces = (size_t)s.ch * tensors * (dtype_size(d->x_dtype) + dtype_size(d->b_dtype)) / 2;
+    return (tensors == 1 ? 3 : 2) * 16 * (pieces | 1) * (size_t)s.threads;
+}
+// A thread takes sixteen columns, eight where the rings of two blocks would not fit an SM, and 32 (without a ring) beyond 8192.
+static JoinShape join_shape(const qbp_resnorm_desc *d, int tensors)
+{
+    const int chunks = (int)((d->cols + 255) / 256);                 // a warp's eight columns a lane
+    if (chunks <= 1) return {1, 32 * kJoinWarpRows, true};
+    if (chunks <= 2) return {2, 32 * kJoinWarpRows, true};
+    JoinShape s{2, 32 * ((chunks + 1) / 2), false};
+    if (s.threads > 128 && chunks <= 16 && 2 * join_ring(d, s, tensors) > kJoinSmRings) s = {1, 32 * chunks, false};
+    if (s.threads <= 512 && join_ring(d, s, tensors) <= kJoinMaxRing) return s;
+    return {4, 32 * ((chunks + 3) / 4), false};
 }
 
-#define QBP_FOR_JOIN(shape, CH, WARP, call)                                                          \
-    do {                                                                                             \
-        if ((shape).warp) {                                                                          \
-            constexpr bool WARP = true;                                                              \
-            if ((shape).ch == 1) { constexpr int CH = 1; call; }                                     \
-            else if ((shape).ch == 2) { constexpr int CH = 2; call; }                                \
-            else { constexpr int CH = 4; call; }                                                     \
-        } else {                                                                                     \
-            constexpr bool WARP = false;                                                             \
-            if ((shape).ch == 2) { constexpr int CH = 2; call; }                                     \
-            else { constexpr int CH = 4; call; }                                                     \
-        }                                                                                            \
+// Runs `call` with the kernel's compile-time choices for rows that are read in vectors.
+#define QBP_FOR_JOIN(shape, CH, WARP, call)                                                                                   \
+    do {                                                                                                                      \
+        if ((shape).warp && (shape).ch == 1) { constexpr int CH = 1; constexpr bool WARP = true; call; }                      \
+        else if ((shape).warp) { constexpr int CH = 2; constexpr bool WARP = true; call; }                                    \
+        else if ((shape).ch == 1) { constexpr int CH = 1; constexpr bool WARP = false; call; }                                \
+        else { constexpr int CH = 2; constexpr bool WARP = false; call; }                                                     \
     } while (0)
+
+// Launches with the ring's shared memory.
+template <typename Params>
+static int launch_join(void (*kernel)(Params, PhiloxKeys), PerDeviceOnce &once, int64_t blocks, const JoinShape &s, size_t smem, cudaStream_t st, const Params &P,
+                       const PhiloxKeys &keys)
+{
+    if (smem > 24 * 1024) QBP_SMEM_OPT_IN(once, kernel, kJoinMaxRing);       // (with the static arrays beside it, over 48 KB)
+    launch(kernel, dim3((unsigned)blocks), s.threads, smem, st, P, keys);
+    return QBP_OK;
+}
 
 static int check_join(const qbp_resnorm_desc *d, const char *name, const void *b, const float *gate, const float *w_post, const float *w_pre)
 {
@@ -351,8 +824,35 @@ static int check_join(const qbp_resnorm_desc *d, const char *name, const void *b
     return QBP_OK;
 }
 static bool real_ok(const void *p, int dtype) { return p && aligned_to(p, dtype_size(dtype)); }
-static bool rows_vec(const void *p, int dtype, int64_t cols) { return aligned16(p) && cols * (int64_t)dtype_size(dtype) % 16 == 0; }
 static int64_t join_gates(const qbp_resnorm_desc *d) { return d->gate_rows ? (d->rows + d->gate_rows - 1) / d->gate_rows : 1; }
+
+// How the rows are cut for a grid of at most `most` blocks: items of neighbouring rows of one gate.
+struct JoinCut { JoinItems it; int64_t blocks; };
+static JoinCut join_cut(const qbp_resnorm_desc *d, const JoinShape &s, bool per_gate, int64_t most, int64_t few)
+{
+    JoinCut c{};
+    JoinItems &it = c.it;
+    it.rows = d->rows; it.cols = d->cols;
+    it.gates = per_gate && d->gate_rows ? join_gates(d) : 1;
+    it.gate_rows = per_gate && d->gate_rows ? d->gate_rows : std::max<int64_t>(d->rows, 1);
+    if (s.warp) few *= kJoinWarpRows;                                // a block takes so many rows at a time
+    it.splits = std::max<int64_t>(1, std::min((most + it.gates - 1) / it.gates, (it.gate_rows + few - 1) / few));
+    it.split_rows = (it.gate_rows + it.splits - 1) / it.splits;
+    it.splits = (it.gate_rows + it.split_rows - 1) / it.split_rows;
+    c.blocks = std::min(most, it.gates * it.splits);
+    return c;
+}
+// Blocks of a wave: 16 warps an SM (8 backwards where a row is a warp's), which their registers allow, or what their rings leave room for.
+static int64_t join_blocks(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
+{
+    const int64_t per_sm = std::min<int64_t>((s.warp && tensors == 2 ? 256 : 512) / s.threads, (int64_t)(227 * 1024 / (join_ring(d, s, tensors) + 2048 + (s.warp ? 16384 : 0))));
+    return (int64_t)sm_count() * std::max<int64_t>(per_sm, 1);
+}
+static JoinCut join_cut_bwd(const qbp_resnorm_desc *d, bool per_gate)
+{
+    const JoinShape s = join_shape(d, 2);
+    return join_cut(d, s, per_gate, join_blocks(d, s, 2), 4);
+}
 
 extern "C" __attribute__((visibility("default"))) int qbp_resnorm_fwd(const qbp_resnorm_desc *d, const void *x, const void *b, const float *w_post,
                                                                       const float *gate, const float *w_pre, void *r, void *h, float *rstd_post,
@@ -367,41 +867,31 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_fwd(const qbp_
     if (!r && (b || d->alpha != 1.0f)) return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: r may be NULL only where it is x");
     if (!r && !d->pre) return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: no output wanted");
     JoinParams P{};
-    P.rows = d->rows; P.cols = d->cols; P.gate_rows = gate ? d->gate_rows : 0;
+    const JoinShape s = join_shape(d, 1);
+    const JoinCut c = join_cut(d, s, gate != nullptr, join_blocks(d, s, 1), 1);
+    P.it = c.it;
     P.x = x; P.b = b; P.w_post = w_post; P.gate = gate; P.w_pre = w_pre; P.r = r; P.h = h; P.rstd_post = rstd_post; P.rstd_pre = rstd_pre;
     P.eps = d->eps; P.alpha = d->alpha; P.inv_cols = (float)(1.0 / (double)d->cols);
-    P.post = d->post ? 1 : 0; P.pre = d->pre ? 1 : 0;
-    P.vec_x = rows_vec(x, d->x_dtype, d->cols) && (!r || aligned16(r)) ? 1 : 0;
-    P.vec_b = rows_vec(b, d->b_dtype, d->cols) && (!h || aligned16(h)) ? 1 : 0;
-    P.vec_w = aligned16(w_post) && aligned16(gate) && aligned16(w_pre) && d->cols % 4 == 0 ? 1 : 0;
+    P.post = d->post ? 1 : 0; P.pre = d->pre ? 1 : 0; P.x_dtype = d->x_dtype; P.b_dtype = d->b_dtype;
     P.d = dropout_params(d->p, d->tensor_id, d->index_base);
-    P.drop = P.d.threshold ? 1 : 0;
+    P.drop = P.d.threshold == 65536u ? 2 : P.d.threshold ? 1 : 0;
+    P.wide = aligned_to(r, 32) && aligned_to(h, 32) ? 1 : 0;
     const PhiloxKeys keys = philox_keys_host(d->seed);
-    const JoinShape s = join_shape(d->cols);
-    const int64_t want = s.warp ? (d->rows + kJoinWarpRows - 1) / kJoinWarpRows : d->rows;
-    const unsigned grid = (unsigned)std::min<int64_t>(want, 8ll * sm_count());
+    const bool vec = d->cols % 8 == 0 && aligned16(x) && aligned16(b) && aligned16(r) && aligned16(h) && aligned16(w_post) && aligned16(gate) && aligned16(w_pre);
     QBP_TRACE_BEGIN(st);
-    QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, CH, WARP, (launch(join_fwd_kernel<TX, TB, CH, WARP>, grid, s.threads, 0, st, P, keys)))));
+    if (vec && s.ch <= 2)
+        QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, CH, WARP, {
+            static PerDeviceOnce once;
+            if ((rc = launch_join(join_fwd_kernel<TX, TB, CH, WARP>, once, c.blocks, s, join_ring(d, s, 1), st, P, keys))) return rc;
+        })));
+    else if (vec)
+        QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, (launch(join_fwd_any_kernel<TX, TB, 4, false, true>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys))));
+    else if (s.ch == 4)
+        launch(join_fwd_any_kernel<AnyReal, AnyReal, 4, false, false>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys);
+    else
+        QBP_FOR_JOIN(s, CH, WARP, (launch(join_fwd_any_kernel<AnyReal, AnyReal, CH, WARP, false>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys)));
     QBP_LAUNCH_OK("join_fwd_kernel");
     return QBP_OK;
-}
-
-// How the backward pass cuts the rows: `blocks` blocks, each gate in `splits` items.
-struct JoinCut { int64_t blocks, splits, split_rows, gates, gate_rows; };
-static JoinCut join_cut(const qbp_resnorm_desc *d, bool per_gate)
-{
-    JoinCut c;
-    const JoinShape s = join_shape(d->cols);
-    c.gates = per_gate ? join_gates(d) : 1;
-    c.gate_rows = per_gate && d->gate_rows ? d->gate_rows : std::max<int64_t>(d->rows, 1);
-    const int64_t most = 2ll * sm_count();
-    // a warp's row costs a quarter of a block's, and a block of warps takes eight at a time
-    const int64_t few = s.warp ? 2 * kJoinWarpRows : 2;
-    c.splits = std::max<int64_t>(1, std::min((most + c.gates - 1) / c.gates, (c.gate_rows + few - 1) / few));
-    c.split_rows = (c.gate_rows + c.splits - 1) / c.splits;
-    c.splits = (c.gate_rows + c.split_rows - 1) / c.split_rows;
-    c.blocks = std::min(most, c.gates * c.splits);
-    return c;
 }
 
 extern "C" __attribute__((visibility("default"))) size_t qbp_resnorm_bwd_workspace_bytes(const qbp_resnorm_desc *d)
@@ -409,8 +899,8 @@ extern "C" __attribute__((visibility("default"))) size_t qbp_resnorm_bwd_workspa
     if (!d || d->rows <= 0 || d->cols <= 0) return 256;
     size_t most = 0;
     for (bool per_gate : {false, true}) {
-        const JoinCut c = join_cut(d, per_gate);
-        most = std::max(most, 2 * align_up((size_t)(c.blocks * d->cols) * 4, 256) + align_up((size_t)(c.gates * c.splits * d->cols) * 4, 256));
+        const JoinCut c = join_cut_bwd(d, per_gate);
+        most = std::max(most, 2 * align_up((size_t)(c.blocks * d->cols) * 4, 256) + align_up((size_t)(c.it.gates * c.it.splits * d->cols) * 4, 256));
     }
     return 256 + most;
 }
@@ -442,38 +932,46 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
     if (!dr && !d->pre) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: neither output has a gradient");
     if (!ws || !aligned_to(ws, 256) || ws_bytes < qbp_resnorm_bwd_workspace_bytes(d))
         return fail(QBP_ERR_WORKSPACE, "resnorm_bwd: workspace NULL, misaligned or smaller than %zu bytes", qbp_resnorm_bwd_workspace_bytes(d));
-    const bool per_gate = gate || dgate;
-    const JoinCut c = join_cut(d, per_gate && d->gate_rows > 0);
+    const JoinCut c = join_cut_bwd(d, gate || dgate);
+    const int64_t items = c.it.gates * c.it.splits;
     WsCarver w(ws, ws_bytes);
     JoinBwdParams P{};
-    P.rows = d->rows; P.cols = d->cols; P.gate_rows = c.gate_rows; P.gates = c.gates; P.splits = c.splits; P.split_rows = c.split_rows;
+    P.it = c.it;
     P.dr = dr; P.dh = dh; P.b = b; P.r = r; P.rstd_post = rstd_post; P.rstd_pre = rstd_pre; P.w_post = w_post; P.gate = gate; P.w_pre = w_pre;
     P.dx = dx; P.db = db; P.alpha = d->alpha; P.inv_cols = (float)(1.0 / (double)d->cols);
-    P.post = d->post ? 1 : 0; P.pre = d->pre ? 1 : 0;
+    P.post = d->post ? 1 : 0; P.pre = d->pre ? 1 : 0; P.x_dtype = d->x_dtype; P.b_dtype = d->b_dtype;
     P.part_post = w.take<float>((size_t)(c.blocks * d->cols)); P.part_pre = w.take<float>((size_t)(c.blocks * d->cols));
-    P.part_gate = w.take<float>((size_t)(c.gates * c.splits * d->cols));
+    P.part_gate = w.take<float>((size_t)(items * d->cols));
     P.sum_post = dw_post ? 1 : 0; P.sum_pre = dw_pre ? 1 : 0; P.sum_gate = dgate ? 1 : 0;
-    if (dgate && c.splits == 1) P.part_gate = dgate;
+    if (dgate && c.it.splits == 1) P.part_gate = dgate;
     if (dw_post && c.blocks == 1) P.part_post = dw_post;
     if (dw_pre && c.blocks == 1) P.part_pre = dw_pre;
-    const auto vec = [&](const void *p) { return aligned16(p); };
-    P.vec_x = vec(dr) && vec(r) && vec(dx) && d->cols * (int64_t)dtype_size(d->x_dtype) % 16 == 0 ? 1 : 0;
-    P.vec_b = vec(dh) && vec(b) && vec(db) && d->cols * (int64_t)dtype_size(d->b_dtype) % 16 == 0 ? 1 : 0;
-    P.vec_w = vec(w_post) && vec(gate) && vec(w_pre) && d->cols % 4 == 0 ? 1 : 0;
     P.d = dropout_params(d->p, d->tensor_id, d->index_base);
-    P.drop = P.d.threshold ? 1 : 0;
+    P.drop = P.d.threshold == 65536u ? 2 : P.d.threshold ? 1 : 0;
+    P.wide = aligned_to(dx, 32) && aligned_to(db, 32) ? 1 : 0;
     const PhiloxKeys keys = philox_keys_host(d->seed);
-    const JoinShape s = join_shape(d->cols);
-    const size_t smem = s.warp ? (size_t)kJoinWarpRows * align_up((size_t)d->cols, 8) * 4 : 0;           // at most 32 KB
+    const JoinShape s = join_shape(d, 2);
+    const bool vec = d->cols % 8 == 0 && aligned16(dr) && aligned16(dh) && aligned16(b) && aligned16(r) && aligned16(dx) && aligned16(db) && aligned16(w_post) &&
+                     aligned16(gate) && aligned16(w_pre);
     QBP_TRACE_BEGIN(st);
-    QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, CH, WARP, (launch(join_bwd_kernel<TX, TB, CH, WARP>, (unsigned)c.blocks, s.threads, smem, st, P, keys)))));
+    if (vec && s.ch <= 2)
+        QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, CH, WARP, {
+            static PerDeviceOnce once;
+            if ((rc = launch_join(join_bwd_kernel<TX, TB, CH, WARP>, once, c.blocks, s, join_ring(d, s, 2), st, P, keys))) return rc;
+        })));
+    else if (vec)
+        QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, (launch(join_bwd_any_kernel<TX, TB, 4, false, true>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys))));
+    else if (s.ch == 4)
+        launch(join_bwd_any_kernel<AnyReal, AnyReal, 4, false, false>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys);
+    else
+        QBP_FOR_JOIN(s, CH, WARP, (launch(join_bwd_any_kernel<AnyReal, AnyReal, CH, WARP, false>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys)));
     QBP_LAUNCH_OK("join_bwd_kernel");
     JoinSums S{};
     int jobs = 0;
     int64_t outs = 1;
     if (dw_post && c.blocks > 1) S.j[jobs++] = {P.part_post, dw_post, 1, c.blocks};
     if (dw_pre && c.blocks > 1) S.j[jobs++] = {P.part_pre, dw_pre, 1, c.blocks};
-    if (dgate && c.splits > 1) { S.j[jobs++] = {P.part_gate, dgate, c.gates, c.splits}; outs = c.gates; }
+    if (dgate && c.it.splits > 1) { S.j[jobs++] = {P.part_gate, dgate, c.it.gates, c.it.splits}; outs = c.it.gates; }
     if (!jobs) return QBP_OK;
     S.cols = d->cols;
     QBP_TRACE_BEGIN(st);
