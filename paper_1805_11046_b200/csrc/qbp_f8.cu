@@ -9,122 +9,128 @@ namespace qbp {
 // ================================================================== quantisers
 // A block takes one 128 x 128 tile: thread t holds the eight columns 8 (t % 16) of the rows t / 16 + 16 i in registers, so
 // that x is read once for both copies.  A row's largest magnitude is found by the sixteen lanes that hold it, a column's by a
-// warp's two rows and then across the warps in shared memory.  Magnitudes are compared as integers: that orders NaN above
-// infinity above the finite values, so that one comparison finds a block that is not finite.
+// warp's two rows and then across the warps in shared memory.  The maxima pass a NaN on; a block that is not finite gets a NaN for
+// its inverse scale, and with it NaN codes.
 constexpr int kQuantThreads = 256;
 constexpr int kQuantPasses = 8;
 
 enum { kF8Rows = 1, kF8Cols = 2, kF8Square = 4 };
 
-// (the piece's byte of an outer index and a block)
-__device__ __forceinline__ int64_t scale_at(int64_t outer, int64_t block, int64_t groups)
+// The scale byte of outer index `o` (0..127 of the tile's piece) and block `b`; behind the last block, the rest of its word.
+__device__ __forceinline__ void put_scale(uint8_t *piece, int o, int b, bool last, uint32_t byte)
 {
-    return ((outer >> 7) * groups + (block >> 2)) * kF8Piece + (outer & 31) * 16 + ((outer >> 5) & 3) * 4 + (block & 3);
-}
-// The byte of this outer index and block; behind the last block, the rest of its word.
-__device__ __forceinline__ void put_scale(uint8_t *s, int64_t outer, int64_t block, int64_t blocks, uint32_t byte)
-{
-    uint8_t *at = s + scale_at(outer, block, (blocks + 3) >> 2);
-    *at = (uint8_t)byte;
-    if (block == blocks - 1)
-        for (int k = (int)(block & 3) + 1; k < 4; ++k) *++at = 127;
+    uint8_t *at = piece + (o & 31) * 16 + (o >> 5) * 4;
+    if (!last) at[b] = (uint8_t)byte;
+    else {
+        const uint32_t pad = 0x7F7F7F7Fu << (8 * b), word = (byte << (8 * b)) | (b < 3 ? pad << 8 : 0u);
+        for (int k = b; k < 4; ++k) at[k] = (uint8_t)(word >> (8 * k));
+    }
 }
 
 template <typename T, int FORMAT, int WHAT>
-__global__ void __launch_bounds__(kQuantThreads) f8_quantize_kernel(const T *__restrict__ x, int64_t rows, int64_t cols, int64_t ld, int vec,
-                                                                    uint8_t *__restrict__ q_rows, uint8_t *__restrict__ s_rows,
-                                                                    uint8_t *__restrict__ q_cols, uint8_t *__restrict__ s_cols)
+__global__ void __launch_bounds__(kQuantThreads, sizeof(T) == 2 ? 3 : 2)
+f8_quantize_kernel(const T *__restrict__ x, int64_t rows, int64_t cols, int64_t ld, int vec, uint8_t *__restrict__ q_rows, uint8_t *__restrict__ s_rows,
+                   uint8_t *__restrict__ q_cols, uint8_t *__restrict__ s_cols)
 {
-    __shared__ uint32_t s_amax[kQuantThreads / 32][kF8Block];
-    __shared__ uint8_t s_byte[kF8Block];
-    __shared__ uint32_t s_warp[kQuantThreads / 32];
+    __shared__ float s_amax[kQuantThreads / 32][kF8Block];
+    __shared__ float s_inv[kF8Block];
     const int lane16 = threadIdx.x & 15, high = threadIdx.x >> 4, warp = threadIdx.x >> 5;
-    const int64_t tile_c = blockIdx.x, tile_r = blockIdx.y;
-    const int64_t c0 = tile_c * kF8Block + 8 * lane16, r0 = tile_r * kF8Block;
-    const int n = (int)min((int64_t)8, max((int64_t)0, cols - c0));                // 8 or 0: cols is a multiple of 16
+    const int64_t tile_c = blockIdx.x, tile_r = blockIdx.y, r0 = tile_r * kF8Block, c0 = tile_c * kF8Block + 8 * lane16;
+    const int here = (int)min((int64_t)kF8Block, rows - r0);                        // rows of the tile
+    const bool in = c0 < cols;                                                      // (cols is a multiple of 16: all eight or none)
+    // the tile's pieces: of its rows (blocks along the columns) and of its columns
+    const int64_t blocks_c = (cols + 127) >> 7, blocks_r = (rows + 127) >> 7;
+    uint8_t *const p_rows = s_rows + (tile_r * ((blocks_c + 3) >> 2) + (tile_c >> 2)) * kF8Piece;
+    uint8_t *const p_cols = s_cols + (tile_c * ((blocks_r + 3) >> 2) + (tile_r >> 2)) * kF8Piece;
+    const int b_rows = (int)tile_c & 3, b_cols = (int)tile_r & 3;
+    const bool last_c = tile_c == blocks_c - 1, last_r = tile_r == blocks_r - 1;
+    const T *src = x + (r0 + high) * ld + c0;
     pdl_wait();
     Raw8<T> raw[kQuantPasses];
+    if (vec) {
 #pragma unroll
-    for (int i = 0; i < kQuantPasses; ++i) {
-        const int64_t r = r0 + 16 * i + high;
-        raw[i] = load8(x + (r < rows ? r : 0) * ld + (n ? c0 : 0), r < rows ? n : 0, vec != 0);
+        for (int i = 0; i < kQuantPasses; ++i)
+#pragma unroll
+            for (int k = 0; k < (int)(sizeof(T) / 2); ++k)
+                raw[i].w[k] = in && 16 * i + high < here ? __ldg(reinterpret_cast<const uint4 *>(src + 16 * i * ld) + k) : make_uint4(0, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kQuantPasses; ++i) raw[i] = load8(in && 16 * i + high < here ? src + 16 * i * ld : x, in && 16 * i + high < here ? 8 : 0, false);
     }
-    uint32_t col_max[8] = {}, tile_max = 0, row_max[kQuantPasses];
+    float col_max[8] = {}, row_max[kQuantPasses];
 #pragma unroll
     for (int i = 0; i < kQuantPasses; ++i) {
         float v[8];
         unpack8(raw[i], v);
-        uint32_t m = 0;
+        if (WHAT & (kF8Rows | kF8Square)) row_max[i] = amax3(amax3(amax3(amax3(v[0], v[1], v[2]), v[3], v[4]), v[5], v[6]), v[7], 0.0f);
+        if (WHAT & kF8Cols) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t b = __float_as_uint(v[e]) & 0x7FFFFFFFu;
-            m = max(m, b);
-            if (WHAT & kF8Cols) col_max[e] = max(col_max[e], b);
+            for (int e = 0; e < 8; ++e) col_max[e] = amax3(col_max[e], v[e], 0.0f);
         }
-        row_max[i] = m;
-        tile_max = max(tile_max, m);
     }
-    const int64_t blocks_c = (cols + 127) >> 7, blocks_r = (rows + 127) >> 7;
-    uint32_t col_byte[8], tile_byte = 127;
+    float col_inv[8], tile_inv = 1.0f;
     if (WHAT & kF8Cols) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t m = max(col_max[e], __shfl_xor_sync(0xFFFFFFFFu, col_max[e], 16));
-            if ((threadIdx.x & 16) == 0) s_amax[warp][8 * lane16 + e] = m;
+            col_max[e] = amax3(col_max[e], __shfl_xor_sync(0xFFFFFFFFu, col_max[e], 16), 0.0f);
+            if ((threadIdx.x & 16) == 0) s_amax[warp][8 * lane16 + e] = col_max[e];
         }
         __syncthreads();
         if (threadIdx.x < kF8Block) {
-            uint32_t m = 0;
+            float m = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kQuantThreads / 32; ++w) m = max(m, s_amax[w][threadIdx.x]);
-            const uint32_t byte = f8_scale_byte<FORMAT>(m);                        // (127 for columns behind the last)
-            s_byte[threadIdx.x] = (uint8_t)byte;
-            put_scale(s_cols, tile_c * kF8Block + threadIdx.x, tile_r, blocks_r, byte);
+            for (int w = 0; w < kQuantThreads / 32; w += 2) m = amax3(m, s_amax[w][threadIdx.x], s_amax[w + 1][threadIdx.x]);
+            const uint32_t byte = f8_scale_byte<FORMAT>(m);                         // (127 for columns behind the last)
+            s_inv[threadIdx.x] = f8_inverse(byte);
+            put_scale(p_cols, threadIdx.x, b_cols, last_r, byte);
         }
         __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) col_byte[e] = s_byte[8 * lane16 + e];
+        const float4 a = *reinterpret_cast<const float4 *>(s_inv + 8 * lane16), b = *reinterpret_cast<const float4 *>(s_inv + 8 * lane16 + 4);
+        col_inv[0] = a.x; col_inv[1] = a.y; col_inv[2] = a.z; col_inv[3] = a.w; col_inv[4] = b.x; col_inv[5] = b.y; col_inv[6] = b.z; col_inv[7] = b.w;
     }
     if (WHAT & kF8Square) {
-        tile_max = __reduce_max_sync(0xFFFFFFFFu, tile_max);
-        if ((threadIdx.x & 31) == 0) s_warp[warp] = tile_max;
-        __syncthreads();
-        uint32_t m = 0;
+        float m = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kQuantThreads / 32; ++w) m = max(m, s_warp[w]);
-        tile_byte = f8_scale_byte<FORMAT>(m);
+        for (int i = 0; i < kQuantPasses; i += 2) m = amax3(m, row_max[i], row_max[i + 1]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = amax3(m, __shfl_xor_sync(0xFFFFFFFFu, m, o), 0.0f);
+        if ((threadIdx.x & 31) == 0) s_amax[warp][0] = m;
+        __syncthreads();
+        m = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kQuantThreads / 32; w += 2) m = amax3(m, s_amax[w][0], s_amax[w + 1][0]);
+        const uint32_t byte = f8_scale_byte<FORMAT>(m);
+        tile_inv = f8_inverse(byte);
         if (threadIdx.x < kF8Block) {
-            const int64_t r = r0 + threadIdx.x, c = tile_c * kF8Block + threadIdx.x;
-            if (s_rows) put_scale(s_rows, r, tile_c, blocks_c, r < rows ? tile_byte : 127u);
-            if (s_cols) put_scale(s_cols, c, tile_r, blocks_r, c < cols ? tile_byte : 127u);
+            if (s_rows) put_scale(p_rows, threadIdx.x, b_rows, last_c, (int)threadIdx.x < here ? byte : 127u);
+            if (s_cols) put_scale(p_cols, threadIdx.x, b_cols, last_r, tile_c * kF8Block + threadIdx.x < cols ? byte : 127u);
         }
     }
+    uint8_t *const d_rows = q_rows + (r0 + high) * cols + c0, *const d_cols = q_cols + (r0 + high) * cols + c0;
 #pragma unroll
     for (int i = 0; i < kQuantPasses; ++i) {
-        const int64_t r = r0 + 16 * i + high;
-        float v[8];
+        const int r = 16 * i + high;
+        float v[8], inv = tile_inv;
         unpack8(raw[i], v);
-        uint32_t byte = tile_byte;
         if (WHAT & kF8Rows) {
-            uint32_t m = row_max[i];
+            float m = row_max[i];
 #pragma unroll
-            for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-            byte = f8_scale_byte<FORMAT>(m);
-            if (lane16 == 0) put_scale(s_rows, r, tile_c, blocks_c, byte);           // (127 for rows behind the last)
+            for (int o = 8; o > 0; o >>= 1) m = amax3(m, __shfl_xor_sync(0xFFFFFFFFu, m, o), 0.0f);
+            const uint32_t byte = f8_scale_byte<FORMAT>(m);
+            inv = f8_inverse(byte);
+            if (lane16 == 0) put_scale(p_rows, r, b_rows, last_c, byte);              // (127 for rows behind the last)
         }
-        if (r < rows && n) {
-            if (WHAT & (kF8Rows | kF8Square))
-                *reinterpret_cast<uint2 *>(q_rows + r * cols + c0) = f8_codes8<FORMAT>(v, f8_inverse(byte), byte == 255u);
-            if (WHAT & kF8Cols) {
+        if (r < here && in) {
+            if (WHAT & (kF8Rows | kF8Square)) {
                 float t[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) t[e] = __fmul_rn(v[e], f8_inverse(col_byte[e]));
-                uint2 c = f8_codes8<FORMAT>(t, 1.0f, false);
-                uint8_t *b = reinterpret_cast<uint8_t *>(&c);
+                for (int e = 0; e < 8; ++e) t[e] = __fmul_rn(v[e], inv);
+                *reinterpret_cast<uint2 *>(d_rows + 16 * i * cols) = f8_codes8<FORMAT>(t);
+            }
+            if (WHAT & kF8Cols) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (col_byte[e] == 255u) b[e] = (uint8_t)kF8Nan;
-                *reinterpret_cast<uint2 *>(q_cols + r * cols + c0) = c;
+                for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], col_inv[e]);
+                *reinterpret_cast<uint2 *>(d_cols + 16 * i * cols) = f8_codes8<FORMAT>(v);
             }
         }
     }

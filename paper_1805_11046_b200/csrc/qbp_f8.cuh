@@ -48,7 +48,6 @@ int launch_f8_pair(const F8Product &p, cudaStream_t st);
 template <int FORMAT> struct F8Format;
 template <> struct F8Format<QBP_E4M3> { static constexpr int top = 8; };
 template <> struct F8Format<QBP_E5M2> { static constexpr int top = 15; };
-constexpr uint32_t kF8Nan = 0x7Fu;                                // a NaN in either format
 
 // Two values to codes, nearest with ties to even, saturating; the first in the low byte.
 template <int FORMAT> __device__ __forceinline__ uint32_t f8_codes2(float a, float b)
@@ -58,24 +57,29 @@ template <int FORMAT> __device__ __forceinline__ uint32_t f8_codes2(float a, flo
     else                    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
     return r;
 }
-// The scale byte of a block from the bits of its largest magnitude: the smallest e >= -127 with amax <= 1.75 * 2^(top + e); 127
-// (a scale of one) for a block of zeros, 255 where a value is infinite or not a number.
-template <int FORMAT> __device__ __forceinline__ uint32_t f8_scale_byte(uint32_t amax_bits)
+// Largest magnitude of three; NaN if one of them is.
+__device__ __forceinline__ float amax3(float a, float b, float c)
 {
-    if (amax_bits >= 0x7F800000u) return 255u;
-    if (amax_bits == 0u) return 127u;
-    const int e = (int)(amax_bits >> 23) - 127 - F8Format<FORMAT>::top + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    float d;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// The scale byte of a block from its largest magnitude: the smallest e >= -127 with amax <= 1.75 * 2^(top + e); 127 (a scale of
+// one) for a block of zeros, 255 where a value is infinite or not a number.
+template <int FORMAT> __device__ __forceinline__ uint32_t f8_scale_byte(float amax)
+{
+    const uint32_t bits = __float_as_uint(amax) & 0x7FFFFFFFu;
+    if (bits >= 0x7F800000u) return 255u;
+    if (bits == 0u) return 127u;
+    const int e = (int)(bits >> 23) - 127 - F8Format<FORMAT>::top + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
     return (uint32_t)(max(e, -127) + 127);
 }
-// 2^-e of a finite scale byte (e <= 120: a normal number, up to 2^127)
-__device__ __forceinline__ float f8_inverse(uint32_t byte) { return __uint_as_float((254u - min(byte, 253u)) << 23); }
-// Eight values to eight codes with one inverse scale; nan: the block holds a value that is not finite.
-template <int FORMAT> __device__ __forceinline__ uint2 f8_codes8(const float (&v)[8], float inv, bool nan)
+// 2^-e of a scale byte (e <= 120: a normal number, up to 2^127; NaN of 255)
+__device__ __forceinline__ float f8_inverse(uint32_t byte) { return byte == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((254u - byte) << 23); }
+// Eight scaled values to eight codes (a NaN to the format's NaN).
+template <int FORMAT> __device__ __forceinline__ uint2 f8_codes8(const float (&v)[8])
 {
-    uint2 r;
-    r.x = f8_codes2<FORMAT>(__fmul_rn(v[0], inv), __fmul_rn(v[1], inv)) | (f8_codes2<FORMAT>(__fmul_rn(v[2], inv), __fmul_rn(v[3], inv)) << 16);
-    r.y = f8_codes2<FORMAT>(__fmul_rn(v[4], inv), __fmul_rn(v[5], inv)) | (f8_codes2<FORMAT>(__fmul_rn(v[6], inv), __fmul_rn(v[7], inv)) << 16);
-    return nan ? make_uint2(kF8Nan * 0x01010101u, kF8Nan * 0x01010101u) : r;
+    return make_uint2(f8_codes2<FORMAT>(v[0], v[1]) | (f8_codes2<FORMAT>(v[2], v[3]) << 16), f8_codes2<FORMAT>(v[4], v[5]) | (f8_codes2<FORMAT>(v[6], v[7]) << 16));
 }
 
 __device__ __forceinline__ void tma_load_3d(void *dst, const void *map, uint64_t *bar, int x, int y, int z)

@@ -130,6 +130,7 @@ def test_a_block_that_is_not_finite_is_nan_and_no_other(B, bad):
     xt, wt = torch.from_numpy(x).cuda(), torch.from_numpy(w).cuda()
     q, s, qc, sc = B.qbp_quantize_f8(xt, cols=True)
     ex = host(B.qbp_f8_exponents(s, M, K)); assert (ex == 128).sum() == 1 and ex[17, 2] == 128
+    assert (host(q)[17, 256:384] == 0x7F).all()
     exc = host(B.qbp_f8_exponents(sc, K, M)); assert (exc == 128).sum() == 1 and exc[300, 0] == 128
     wq, ws, wsc = B.qbp_quantize_f8_square(wt)
     y = host(B.qbp_gemm_f8(q, s, wq, ws, transB=True))
