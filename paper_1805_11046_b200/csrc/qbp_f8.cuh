@@ -20,8 +20,8 @@ inline int64_t f8_groups(int64_t k) { return (k + 511) / 512; }
 
 // Scales as 128 words x groups x tiles of 128 outer indices, read in boxes of `tiles` pieces (qbp_mma.cu).
 int make_map_scales(CUtensorMap *map, const void *base, uint64_t outer, uint64_t K, uint32_t tiles);
-// Output [rows x cols] of 4- or 2-byte elements stored in boxes of 32 x 32, swizzled by 128 or 64 bytes (qbp_mma.cu).
-int make_map_out_32(CUtensorMap *map, void *base, uint64_t rows, uint64_t cols, int dtype);
+// Output [rows x cols] of 4- or 2-byte elements stored in boxes of 32 rows of 64 bytes, swizzled alike (qbp_mma.cu).
+int make_map_out_rows64(CUtensorMap *map, void *base, uint64_t rows, uint64_t cols, int dtype);
 
 // Instruction descriptor of kind::mxf8f6f4: A / B type in bits 7..9 / 10..12 (0 = e4m3, 1 = e5m2), majors in 15 / 16, N >> 3 in
 // 17..22, power-of-two scales in 23, M >> 4 in 24..28; the byte of a scale's word in 4..5 (B) and 29..30 (A).

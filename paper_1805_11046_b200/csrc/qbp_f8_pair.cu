@@ -8,8 +8,17 @@
 // scales cost the tensor pipe nothing then: they are powers of two and the MMA applies them.
 //
 // Tensor memory (512 columns).  Two accumulators of 256 columns would leave none for the scales, so of bn = 256 the second begins
-// at column 224: the last 32 columns of one are the first 32 of the other.  The epilogue of a tile takes these 32 out first, and
-// the next tile's MMAs wait for no more than that.  [480, 504) then holds two sets of scales of 12 columns.
+// at column 192: the last 64 columns of one are the first 64 of the other.  The epilogue of a tile takes these out first, and
+// the next tile's MMAs wait for no more than that.  [448, 508) then holds five sets of scales of 12 columns.
+//
+// A set is written again without a wait of its own.  Of bn = 256 a tile starts when all MMAs before it are done (its accumulator shares
+// columns with the last one), and within a tile five sets are at least 17 blocks apart; of bn = 128 a tile starts when all but the last tile's
+// are done, and eight sets are more than 24 blocks apart within two tiles.  That is more than a ring and a release group: the stage of a
+// block has been filled, so the MMAs of the block that had it before are done.
+//
+// The issuing thread's own time counts: a block's four MMAs are 512 cycles, and with a commit for every block, a wait for its stage that began
+// when its MMAs were due and a barrier for the scales' sets the loop took 740.  Stages are released two at a time, and a stage's barrier
+// is asked while the MMAs before it are being issued.
 //
 // Roles per CTA: warp 0 loads by TMA, warp 1 (first CTA) issues copies of scales and MMAs, warps 2..9 drain the accumulator
 // and store.  Every wait is bounded; on expiry the CTA raises the status word and leaves through the normal exit.  No TMA load
@@ -25,8 +34,8 @@ constexpr int kFpThreads = 320;
 constexpr int kFpEpiWarps = 8;
 constexpr int kFpMaxStages = 8;
 constexpr int kFpGroupM = 8;                     // tiles walk down eight tile rows before moving one column right
-constexpr int kFpMaxSets = 4;
-constexpr uint32_t kFpSlab = 32 * 128;           // staging of a warp: 32 x 32 outputs
+constexpr uint32_t kFpRelease = 2;               // stages released by one commit
+constexpr uint32_t kFpSlab = 32 * 64;            // staging of a warp: 32 rows of 64 bytes
 constexpr uint32_t kFpSmem = 225u * 1024u;
 
 struct F8PairParams {
@@ -35,7 +44,7 @@ struct F8PairParams {
     uint32_t idesc, stage_bytes;
     int bn, stages, k_blocks;
     uint32_t buf1, set_col, set_cols, sets;      // first column of the second accumulator, of the scales; columns of a set
-    int overlap;                                 // the accumulators share 32 columns
+    int overlap;                                 // the accumulators share 64 columns
     int tiles_m, tiles_n, tiles_total, pairs;
     FastDiv d_group;
     int64_t M, N;
@@ -63,9 +72,9 @@ __device__ __forceinline__ FpTile fp_tile(const F8PairParams &P, int tile)
 }
 
 struct FpMmaArgs {
-    uint64_t *full_bar, *empty_bar, *set_bar, *acc_full, *acc_free;
+    uint64_t *full_bar, *empty_bar, *acc_full, *acc_free;
     uint32_t ring, stage_bytes, a_bytes, b_bytes, tmem, a_desc_lo, b_desc_lo, idesc, buf1, set_col, set_cols, sets, stages;
-    int k_blocks, tile0, tiles_total, tile_step;
+    int k_blocks, tile0, tiles_total, tile_step, overlap;
 };
 
 // The issuing warp's loop; false when a wait ran out.  AK, BK: start-address steps (16-byte units) of 32 reduction bytes in the operands'
@@ -75,20 +84,25 @@ __device__ __forceinline__ bool fp_mma_loop(const FpMmaArgs &A)
 {
     constexpr uint32_t a_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
     constexpr uint32_t b_hi = ((8u * RB) >> 4) | (1u << 14) | ((RB == 128 ? 2u : 4u) << 29);
-    uint32_t s = 0, ph = 0, buf = 0, fph = 1, set = 0, sph = 1, at = A.ring;
+    uint32_t s = 0, ph = 0, buf = 0, fph = 1, set = 0, at = A.ring, in_group = 0, group = 0;
+    bool ready = false;                              // this lane has seen the next stage filled
     for (int tile = A.tile0; tile < A.tiles_total; tile += A.tile_step) {
-        if (!mbar_wait_uniform(A.acc_free, fph)) return false;
-        fph ^= 1u;
+        if (!mbar_wait_uniform(&A.acc_free[A.overlap ? 0u : buf], fph)) return false;
+        if (A.overlap || buf == 1u) fph ^= 1u;
         tc_fence_after();
         const uint32_t d_tmem = A.tmem + buf * A.buf1;
         uint32_t t_sa = 0;
         for (int kb = 0; kb < A.k_blocks; ++kb) {
-            if (!mbar_wait_uniform(&A.full_bar[s], ph)) return false;
+            if (!__all_sync(0xffffffffu, ready) && !mbar_wait_uniform(&A.full_bar[s], ph)) return false;
             tc_fence_after();
+            const uint32_t here = at;
+            at += A.stage_bytes;
+            if (++s == A.stages) { s = 0; ph ^= 1u; at = A.ring; }
+            ready = mbar_try_wait(&A.full_bar[s], ph);
             if ((kb & 3) == 0) {
-                if (!mbar_wait_uniform(&A.set_bar[set], sph)) return false;      // the MMAs that read this set are done
+                set = set + 1 == A.sets ? 0u : set + 1;
                 t_sa = A.tmem + A.set_col + set * A.set_cols;
-                const uint32_t scales = at + A.a_bytes + A.b_bytes;
+                const uint32_t scales = here + A.a_bytes + A.b_bytes;
                 if (elect_one()) {
                     copy_piece_pair(t_sa, piece_desc(scales));
 #pragma unroll
@@ -96,19 +110,17 @@ __device__ __forceinline__ bool fp_mma_loop(const FpMmaArgs &A)
                 }
             }
             const uint32_t id = (uint32_t)(kb & 3), idesc = A.idesc | (id << 4) | (id << 29);
-            const uint32_t a_lo = ((at >> 4) & 0x3FFFu) | A.a_desc_lo, b_lo = (((at + A.a_bytes) >> 4) & 0x3FFFu) | A.b_desc_lo;
+            const uint32_t a_lo = ((here >> 4) & 0x3FFFu) | A.a_desc_lo, b_lo = (((here + A.a_bytes) >> 4) & 0x3FFFu) | A.b_desc_lo;
 #pragma unroll
             for (uint32_t kk = 0; kk < 4; ++kk)
                 if (elect_one())
                     mma_f8_pair(d_tmem, ((uint64_t)a_hi << 32) | (uint64_t)(a_lo + kk * AK), ((uint64_t)b_hi << 32) | (uint64_t)(b_lo + kk * BK),
                                 idesc, t_sa, t_sa + 4u, kk == 0 && kb == 0 ? 0u : 1u);
-            if (elect_one()) mma_commit_pair(&A.empty_bar[s]);
-            if ((kb & 3) == 3 || kb == A.k_blocks - 1) {
-                if (elect_one()) mma_commit_pair(&A.set_bar[set]);
-                if (++set == A.sets) { set = 0; sph ^= 1u; }
+            if (++in_group == kFpRelease) {
+                if (elect_one()) mma_commit_pair(&A.empty_bar[group]);
+                in_group = 0;
+                if (++group * kFpRelease == A.stages) group = 0;
             }
-            at += A.stage_bytes;
-            if (++s == A.stages) { s = 0; ph ^= 1u; at = A.ring; }
         }
         if (elect_one()) mma_commit_pair(&A.acc_full[buf]);
         buf ^= 1u;
@@ -116,15 +128,16 @@ __device__ __forceinline__ bool fp_mma_loop(const FpMmaArgs &A)
     return true;
 }
 
-// 32 accumulators of this lane's row as they are stored: 128 or 64 bytes of a swizzled slab row.
-template <typename T> __device__ __forceinline__ void fp_slab_halves(uint8_t *rowp, int lane, const uint32_t (&r)[32])
+// Accumulators of this lane's row as they are stored, 64 bytes of a swizzled slab row: 16 of fp32 or 32 of the halves.
+__device__ __forceinline__ uint4 *fp_slab(uint8_t *slab, int lane, int piece) { return reinterpret_cast<uint4 *>(slab + lane * 64 + ((piece ^ ((lane >> 1) & 3)) << 4)); }
+template <typename T> __device__ __forceinline__ void fp_slab_halves(uint8_t *slab, int lane, const uint32_t (&r)[32])
 {
 #pragma unroll
     for (int j = 0; j < 32; j += 8) {
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r[j + e]);
-        *reinterpret_cast<uint4 *>(rowp + (((j >> 3) ^ ((lane >> 1) & 3)) << 4)) = pack8<T>(v).w[0];
+        *fp_slab(slab, lane, j >> 3) = pack8<T>(v).w[0];
     }
 }
 template <typename T> __device__ __forceinline__ void fp_put(void *out, int64_t at, float v) { static_cast<T *>(out)[at] = real_to<T>(v); }
@@ -132,7 +145,7 @@ template <typename T> __device__ __forceinline__ void fp_put(void *out, int64_t 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFpThreads, 1) f8_pair_kernel(const __grid_constant__ F8PairParams P)
 {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full_bar[kFpMaxStages], empty_bar[kFpMaxStages], set_bar[kFpMaxSets], acc_full[2], acc_free;
+    __shared__ uint64_t full_bar[kFpMaxStages], empty_bar[kFpMaxStages / kFpRelease], acc_full[2], acc_free[2];
     __shared__ uint32_t tmem_slot;
 
     const uint32_t raw_addr = smem_u32(smem_raw);
@@ -143,11 +156,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFpThreads, 1) f8_pa
     const int pair = blockIdx.x >> 1;
 
     if (threadIdx.x == 0) {
-        // "full": the leader's arrive + the bytes of both CTAs; "empty", "set", "acc_full": one multicast commit each;
+        // "full": the leader's arrive + the bytes of both CTAs; "empty" (of a release group) and "acc_full": one multicast commit each;
         // "acc_free" (the leader's is the one waited on): eight warps of each CTA
-        for (int s = 0; s < P.stages; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
-        for (int s = 0; s < kFpMaxSets; ++s) mbar_init(&set_bar[s], 1);
-        mbar_init(&acc_full[0], 1); mbar_init(&acc_full[1], 1); mbar_init(&acc_free, 2 * kFpEpiWarps);
+        for (int s = 0; s < P.stages; ++s) mbar_init(&full_bar[s], 1);
+        for (int g = 0; g < P.stages / (int)kFpRelease; ++g) mbar_init(&empty_bar[g], 1);
+        for (int b = 0; b < 2; ++b) { mbar_init(&acc_full[b], 1); mbar_init(&acc_free[b], 2 * kFpEpiWarps); }
         mbar_fence_init();
         tma_prefetch_desc(&P.mapA); tma_prefetch_desc(&P.mapB); tma_prefetch_desc(&P.mapSA); tma_prefetch_desc(&P.mapSB);
         if (P.tma_out) tma_prefetch_desc(&P.mapC);
@@ -164,34 +177,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFpThreads, 1) f8_pa
     if (P.clear && blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;
 
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t s = 0, ph = 1;
-            const uint32_t operand_bytes = 2u * (P.a.tile_bytes + P.b.tile_bytes), scale_bytes = 2u * (uint32_t)kF8Piece * (1u + (uint32_t)(P.bn >> 7));
-            for (int tile = pair; tile < P.tiles_total && !timed_out; tile += P.pairs) {
-                const FpTile o = fp_tile(P, tile);
-                const int m_mine = o.m0 + 128 * (int)rank, n_mine = o.n0 + (P.bn >> 1) * (int)rank;
-                for (int kb = 0; kb < P.k_blocks; ++kb) {
-                    if (!mbar_wait(&empty_bar[s], ph)) { timed_out = true; break; }
-                    uint8_t *sa = smem + (size_t)s * P.stage_bytes, *sb = sa + P.a.tile_bytes, *scales = sb + P.b.tile_bytes;
-                    const uint32_t bar = map_to_cta(&full_bar[s], 0);
-                    const bool with_scales = (kb & 3) == 0;
+        // (the whole warp in step, an elected lane issues: addresses and coordinates then stay in uniform registers, where the copies
+        // want them; by one lane of a divergent warp a block's two copies took 500 cycles, as long as its MMAs)
+        uint32_t s = 0, ph = 1, in_group = 0, group = 0;
+        const uint32_t operand_bytes = 2u * (P.a.tile_bytes + P.b.tile_bytes), scale_bytes = 2u * (uint32_t)kF8Piece * (1u + (uint32_t)(P.bn >> 7));
+        const uint32_t full0 = map_to_cta(&full_bar[0], 0);
+        const bool a_k = P.a.major == 0, b_k = P.b.major == 0;
+        for (int tile = pair; tile < P.tiles_total && !timed_out; tile += P.pairs) {
+            const FpTile o = fp_tile(P, tile);
+            const int m_mine = o.m0 + 128 * (int)rank, n_mine = o.n0 + (P.bn >> 1) * (int)rank;
+            for (int kb = 0; kb < P.k_blocks; ++kb) {
+                if (in_group == 0 && !mbar_wait_uniform(&empty_bar[group], ph)) { timed_out = true; break; }
+                if (++in_group == kFpRelease) { in_group = 0; ++group; }
+                uint8_t *sa = smem + (size_t)s * P.stage_bytes, *sb = sa + P.a.tile_bytes, *scales = sb + P.b.tile_bytes;
+                const uint32_t bar = full0 + 8u * s;
+                const bool with_scales = (kb & 3) == 0;
+                const int k0 = kb * 128;
+                if (elect_one()) {
                     if (rank == 0) mbar_expect_tx(&full_bar[s], operand_bytes + (with_scales ? scale_bytes : 0u));
-                    if (P.a.major == 0) tma_load_2d_pair(sa, &P.mapA, bar, kb * 128, m_mine);
-                    else                tma_load_2d_pair(sa, &P.mapA, bar, m_mine, kb * 128);
-                    if (P.b.major == 0) tma_load_2d_pair(sb, &P.mapB, bar, kb * 128, n_mine);
-                    else                tma_load_2d_pair(sb, &P.mapB, bar, n_mine, kb * 128);
+                    tma_load_2d_pair(sa, &P.mapA, bar, a_k ? k0 : m_mine, a_k ? m_mine : k0);
+                    tma_load_2d_pair(sb, &P.mapB, bar, b_k ? k0 : n_mine, b_k ? n_mine : k0);
                     if (with_scales) {
                         tma_load_3d_pair(scales, &P.mapSA, bar, 0, kb >> 2, m_mine >> 7);
                         tma_load_3d_pair(scales + kF8Piece, &P.mapSB, bar, 0, kb >> 2, o.n0 >> 7);
                     }
-                    if (++s == (uint32_t)P.stages) { s = 0; ph ^= 1u; }
                 }
+                __syncwarp();
+                if (++s == (uint32_t)P.stages) { s = 0; ph ^= 1u; group = 0; }
             }
         }
     } else if (warp == 1) {
         if (rank == 0) {
             FpMmaArgs A;
-            A.full_bar = full_bar; A.empty_bar = empty_bar; A.set_bar = set_bar; A.acc_full = acc_full; A.acc_free = &acc_free;
+            A.full_bar = full_bar; A.empty_bar = empty_bar; A.acc_full = acc_full; A.acc_free = acc_free; A.overlap = P.overlap;
             A.ring = smem_u32(smem); A.stage_bytes = P.stage_bytes; A.a_bytes = P.a.tile_bytes; A.b_bytes = P.b.tile_bytes; A.tmem = tmem_base;
             A.a_desc_lo = P.a.desc_lo; A.b_desc_lo = P.b.desc_lo; A.idesc = P.idesc; A.buf1 = P.buf1; A.set_col = P.set_col;
             A.set_cols = P.set_cols; A.sets = P.sets; A.stages = (uint32_t)P.stages;
@@ -210,18 +228,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFpThreads, 1) f8_pa
         // the two groups of four warps take half the columns each
         const int ew = warp - 2, quad = warp & 3, half = ew >> 2;
         uint8_t *slab = staging + (size_t)ew * kFpSlab;
-        const uint32_t leader_free = map_to_cta(&acc_free, 0);
+        const uint32_t leader_free = map_to_cta(&acc_free[0], 0);
         const int per_half = P.bn >> 6;                                       // chunks of 32 columns
         uint32_t buf = 0, fph = 0;
         for (int tile = pair; tile < P.tiles_total; tile += P.pairs) {
             const FpTile o = fp_tile(P, tile);
             const int64_t m_slab = (int64_t)o.m0 + 128 * (int)rank + 32 * quad;
-            // The next tile's MMAs write the accumulator that this warp drained before this one, and the shared columns of this one
-            // (the last of the first accumulator, the first of the second).
-            const bool shares = P.overlap && (buf == 0 ? half == 1 : half == 0);
-            if (!shares) { tc_fence_before(); __syncwarp(); if (lane == 0) mbar_arrive_cluster(leader_free); }
+            // This warp's arrival, one a tile and behind the wait for the tile's MMAs, so that it counts for no other tile.  Shared columns:
+            // the next tile's MMAs write the accumulator that this warp has drained before, and of this one the shared columns (the last of
+            // the first accumulator, the first of the second), two chunks of one half's warps.  Else the accumulator is free once drained.
+            const bool shares = buf == 0 ? half == 1 : half == 0;
+            const int free_at = !P.overlap ? per_half - 1 : shares ? 1 : -1;
+            const uint32_t free_bar = leader_free + (P.overlap ? 0u : 8u * buf);
             if (!timed_out && !mbar_wait_warp(&acc_full[buf], fph)) timed_out = true;
-            if (timed_out && shares) { __syncwarp(); if (lane == 0) mbar_arrive_cluster(leader_free); }
+            if (timed_out || free_at < 0) { tc_fence_before(); __syncwarp(); if (lane == 0) mbar_arrive_cluster(free_bar); }
             if (!timed_out) {
                 tc_fence_after();
                 const uint32_t t_addr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * P.buf1;
@@ -230,42 +250,48 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFpThreads, 1) f8_pa
                     uint32_t r[32];
                     tmem_ld_32x32(t_addr + (uint32_t)c0, r);
                     tmem_ld_wait();
-                    if (shares && i == 0) { tc_fence_before(); __syncwarp(); if (lane == 0) mbar_arrive_cluster(leader_free); }
+                    if (i == free_at) { tc_fence_before(); __syncwarp(); if (lane == 0) mbar_arrive_cluster(free_bar); }
                     if (o.n0 + c0 >= P.N || m_slab >= P.M) continue;
-                    if (lane == 0) tma_store_wait_read();
-                    __syncwarp();
-                    if (P.tma_out) {
-                        if (P.dtype == QBP_F32) {
-                            uint8_t *rowp = slab + lane * 128;
+                    if (P.tma_out && P.dtype == QBP_F32) {
 #pragma unroll
-                            for (int j = 0; j < 32; j += 4)
-                                *reinterpret_cast<uint4 *>(rowp + (((j >> 2) ^ (lane & 7)) << 4)) = make_uint4(r[j], r[j + 1], r[j + 2], r[j + 3]);
-                        } else if (P.dtype == QBP_BF16) {
-                            fp_slab_halves<__nv_bfloat16>(slab + lane * 64, lane, r);
-                        } else {
-                            fp_slab_halves<__half>(slab + lane * 64, lane, r);
+                        for (int h = 0; h < 32; h += 16) {
+                            if (lane == 0) tma_store_wait_read();
+                            __syncwarp();
+#pragma unroll
+                            for (int j = 0; j < 16; j += 4) *fp_slab(slab, lane, j >> 2) = make_uint4(r[h + j], r[h + j + 1], r[h + j + 2], r[h + j + 3]);
+                            fence_proxy_async();
+                            __syncwarp();
+                            if (lane == 0 && o.n0 + c0 + h < P.N) { tma_store_2d(&P.mapC, slab, o.n0 + c0 + h, (int)m_slab); tma_store_commit(); }
                         }
+                    } else if (P.tma_out) {
+                        if (lane == 0) tma_store_wait_read();
+                        __syncwarp();
+                        if (P.dtype == QBP_BF16) fp_slab_halves<__nv_bfloat16>(slab, lane, r);
+                        else                     fp_slab_halves<__half>(slab, lane, r);
                         fence_proxy_async();
                         __syncwarp();
                         if (lane == 0) { tma_store_2d(&P.mapC, slab, o.n0 + c0, (int)m_slab); tma_store_commit(); }
                     } else {
-                        // rows that no TMA store can start on: transposed through the slab, one row at a time
+                        // rows that no TMA store can start on: transposed through the slab sixteen columns at a time, two rows of 16 at once
                         uint32_t *words = reinterpret_cast<uint32_t *>(slab);
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) words[lane * 32 + (j ^ lane)] = r[j];
-                        __syncwarp();
-                        const int64_t n = (int64_t)o.n0 + c0 + lane;
                         const int rows = (int)min((int64_t)32, P.M - m_slab);
-                        for (int k = 0; k < rows; ++k) {
-                            const float v = __uint_as_float(words[k * 32 + (lane ^ k)]);
-                            const int64_t at = (m_slab + k) * P.N + n;
-                            if (n < P.N) {
-                                if (P.dtype == QBP_F32) fp_put<float>(P.out, at, v);
-                                else if (P.dtype == QBP_BF16) fp_put<__nv_bfloat16>(P.out, at, v);
-                                else fp_put<__half>(P.out, at, v);
+#pragma unroll
+                        for (int h = 0; h < 32; h += 16) {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) words[lane * 16 + (j ^ (lane >> 1 & 15))] = r[h + j];
+                            __syncwarp();
+                            const int64_t n = (int64_t)o.n0 + c0 + h + (lane & 15);
+                            for (int k = lane >> 4; k < rows; k += 2) {
+                                const float v = __uint_as_float(words[k * 16 + ((lane & 15) ^ (k >> 1 & 15))]);
+                                const int64_t at = (m_slab + k) * P.N + n;
+                                if (n < P.N) {
+                                    if (P.dtype == QBP_F32) fp_put<float>(P.out, at, v);
+                                    else if (P.dtype == QBP_BF16) fp_put<__nv_bfloat16>(P.out, at, v);
+                                    else fp_put<__half>(P.out, at, v);
+                                }
                             }
+                            __syncwarp();
                         }
-                        __syncwarp();
                     }
                 }
             }
@@ -304,14 +330,14 @@ int launch_f8_pair(const F8Product &p, cudaStream_t st)
     if (rc) return rc;
     if ((rc = make_map_scales(&P.mapSA, p.sA, p.M, p.K, 1)) || (rc = make_map_scales(&P.mapSB, p.sB, p.N, p.K, (uint32_t)P.bn / 128))) return rc;
     P.tma_out = aligned16(p.out) && p.N * (int64_t)dtype_size(p.dtype) % 16 == 0 ? 1 : 0;
-    if (P.tma_out && (rc = make_map_out_32(&P.mapC, p.out, p.M, p.N, p.dtype))) return rc;
+    if (P.tma_out && (rc = make_map_out_rows64(&P.mapC, p.out, p.M, p.N, p.dtype))) return rc;
     P.idesc = make_idesc_f8(p.formatA, p.formatB, P.a.major, P.b.major, 256, (uint32_t)P.bn);
     P.k_blocks = (int)f8_blocks(p.K);
     P.overlap = P.bn == 256 ? 1 : 0;
-    P.buf1 = P.bn == 256 ? 224u : 128u;
-    P.set_col = P.bn == 256 ? 480u : 256u;
+    P.buf1 = P.bn == 256 ? 192u : 128u;
+    P.set_col = P.bn == 256 ? 448u : 256u;
     P.set_cols = P.bn == 256 ? 12u : 8u;
-    P.sets = P.bn == 256 ? 2u : 4u;
+    P.sets = P.bn == 256 ? 5u : 8u;
     P.tiles_m = (int)((p.M + 255) / 256); P.tiles_n = (int)((p.N + P.bn - 1) / P.bn);
     const int64_t total = (int64_t)P.tiles_m * P.tiles_n;
     if (total > (1 << 30)) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "gemm_f8: %lld output tiles", (long long)total);
@@ -320,6 +346,8 @@ int launch_f8_pair(const F8Product &p, cudaStream_t st)
     P.d_group = make_fastdiv(kFpGroupM * P.tiles_n);
     P.stage_bytes = (uint32_t)align_up(P.a.tile_bytes + P.b.tile_bytes + (uint32_t)kF8Piece * (1u + (uint32_t)P.bn / 128u), 1024);   // 34 or 25 KB
     P.stages = std::min<int>(kFpMaxStages, (int)((kFpSmem - 1024 - kFpEpiWarps * kFpSlab) / P.stage_bytes));
+    P.stages -= P.stages % (int)kFpRelease;                          // 6 or 8
+    static_assert(kFpMaxStages + kFpRelease <= 17, "a set of scales is written again while MMAs may read it");
     P.M = p.M; P.N = p.N; P.out = p.out; P.dtype = p.dtype; P.status = p.status; P.clear = p.cleared ? 0 : 1;
     const size_t smem = 1024 + (size_t)P.stages * P.stage_bytes + kFpEpiWarps * kFpSlab;
     static PerDeviceOnce configured;

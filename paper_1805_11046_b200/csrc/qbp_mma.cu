@@ -134,18 +134,18 @@ int make_map_scales(CUtensorMap *map, const void *base, uint64_t outer, uint64_t
     return QBP_OK;
 }
 
-// Output matrix of any real type [rows x cols] stored in boxes of 32 rows x 32 columns: rows of 128 or 64 bytes, swizzled alike.
-int make_map_out_32(CUtensorMap *map, void *base, uint64_t rows, uint64_t cols, int dtype)
+// Output matrix of any real type [rows x cols] stored in boxes of 32 rows of 64 bytes, swizzled alike.
+int make_map_out_rows64(CUtensorMap *map, void *base, uint64_t rows, uint64_t cols, int dtype)
 {
     EncodeTiledFn enc = encode_fn();
     if (!enc) return fail(QBP_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
     const bool wide = dtype == QBP_F32;
     cuuint64_t dims[2] = {cols, rows};
     cuuint64_t strides[1] = {cols * (wide ? 4 : 2)};
-    cuuint32_t box[2] = {32, 32};
+    cuuint32_t box[2] = {wide ? 16u : 32u, 32};
     cuuint32_t estr[2] = {1, 1};
     CUresult r = enc(map, wide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == QBP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                     2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, wide ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                     2, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B,
                      CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return fail(QBP_ERR_CUDA, "cuTensorMapEncodeTiled(output %llu x %llu) failed: %d", (unsigned long long)rows,
                                        (unsigned long long)cols, (int)r);
