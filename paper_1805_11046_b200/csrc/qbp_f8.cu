@@ -165,13 +165,14 @@ static int launch_f8_quantize(const void *x, int dtype, int64_t rows, int64_t co
 // The columns' operand (a layer's weights) is the 128-row side of the MMA and the rows (tokens, 16 to 128 of them) its N
 // side: a token or two then cost an N of 16 and not an M of 128, the accumulator's lanes are neighbouring outputs in memory,
 // and the weights, all that counts when rows are few, are read once, by as many SMs as there are tiles times pieces of the
-// reduction.  The CTAs of a cluster leave their fp32 partial tiles in shared memory and add up a share of the rows each, in the
-// order of the pieces.
+// reduction.  Each CTA of a cluster adds up a share of the rows, in the order of the pieces: the others write their fp32 partial
+// sums of these rows into its shared memory (reading them there took a round trip a row: 128 x 1024 x 512 22.6 us with the launch).
 //
-// Roles: warp 0 loads by TMA, warp 1 copies scales to tensor memory and issues the MMAs, warps 2..5 take the accumulator out.
+// Roles: warp 0 loads by TMA, warp 1 copies scales to tensor memory and issues the MMAs, warps 2..9 take the accumulator out.
 // Every wait is bounded.
-constexpr int kSplitThreads = 192;
+constexpr int kSplitThreads = 320;
 constexpr int kSplitMaxStages = 10;
+constexpr uint32_t kSplitRelease = 2;            // stages released by one commit
 constexpr int kSplitMaxParts = 8;
 constexpr uint32_t kSplitSmem = 220u * 1024u;
 constexpr uint32_t kSplitCols = 256;             // tensor memory: the accumulator in [0, 128), then four sets of 8 columns of scales
@@ -187,35 +188,57 @@ struct F8SplitParams {
     int *status;
 };
 
-template <typename T> __device__ __forceinline__ void split_store(void *out, int64_t at, float v) { static_cast<T *>(out)[at] = real_to<T>(v); }
-__device__ __forceinline__ void split_store(const F8SplitParams &P, int64_t at, float v)
-{
-    if (P.dtype == QBP_F32) split_store<float>(P.out, at, v);
-    else if (P.dtype == QBP_BF16) split_store<__nv_bfloat16>(P.out, at, v);
-    else split_store<__half>(P.out, at, v);
-}
 __device__ __forceinline__ uint32_t cluster_rank()
 {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void cluster_barrier()
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t address_in_cta(uint32_t smem_addr, uint32_t rank)
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ float load_of_cta(uint32_t smem_addr, uint32_t rank)
-{
-    uint32_t at; float v;
+    uint32_t at;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-    return v;
+    return at;
+}
+__device__ __forceinline__ void store_in_cta(uint32_t cluster_addr, uint32_t v)
+{
+    asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
+}
+
+// A warp's 16 rows of the accumulator (rows: those that exist) to the output, n: the lane's column.
+template <typename T> __device__ __forceinline__ void split_put(void *out, int64_t m, int64_t N, int64_t n, int rows, const uint32_t (&r)[16])
+{
+    T *o = static_cast<T *>(out) + m * N + n;
+    if (n < N) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j, o += N)
+            if (j < rows) *o = real_to<T>(__uint_as_float(r[j]));
+    }
+}
+// The sums of a part's rows, `step` apart from row `first` on, added up over the parts and stored.
+template <typename T> __device__ __forceinline__ void split_add(void *out, int64_t m, int64_t N, int64_t n, int first, int step, int rows, int parts, int share, const float *sums)
+{
+    T *o = static_cast<T *>(out) + (m + first) * N + n;
+    if (n < N) {
+#pragma unroll 2
+        for (int j = first; j < rows; j += step, o += step * N) {
+            float v[kSplitMaxParts];
+#pragma unroll
+            for (int q = 0; q < kSplitMaxParts; ++q) v[q] = q < parts ? sums[(q * share + j) * 128] : 0.0f;
+            float t = 0.0f;
+#pragma unroll
+            for (int q = 0; q < kSplitMaxParts; ++q) t += v[q];
+            *o = real_to<T>(t);
+        }
+    }
 }
 
 __global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid_constant__ F8SplitParams P)
 {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full_bar[kSplitMaxStages], empty_bar[kSplitMaxStages], acc_full;
+    __shared__ uint64_t full_bar[kSplitMaxStages], empty_bar[kSplitMaxStages / kSplitRelease], acc_full;
     __shared__ uint32_t tmem_slot;
     const uint32_t raw_addr = smem_u32(smem_raw);
     uint8_t *smem = smem_raw + ((1024u - (raw_addr & 1023u)) & 1023u);
@@ -225,7 +248,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid
     const int kb0 = (int)((int64_t)P.k_blocks * part / P.parts), kb1 = (int)((int64_t)P.k_blocks * (part + 1) / P.parts);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < P.stages; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
+        for (int s = 0; s < P.stages; ++s) mbar_init(&full_bar[s], 1);
+        for (int g = 0; g < P.stages / (int)kSplitRelease; ++g) mbar_init(&empty_bar[g], 1);
         mbar_init(&acc_full, 1);
         mbar_fence_init();
         tma_prefetch_desc(&P.mapU); tma_prefetch_desc(&P.mapV); tma_prefetch_desc(&P.mapSU); tma_prefetch_desc(&P.mapSV);
@@ -236,36 +260,43 @@ __global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     bool timed_out = false;
+    if (P.parts > 1) cluster_arrive();               // (the others' wait for it: this CTA runs, its memory can be written)
     pdl_wait();
     // The status word is cleared here and not by a launch of its own: a wait gives up a second after it began, long after the
     // first block of a grid has started.
     if (P.clear && threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) *P.status = 0;
 
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t s = 0, ph = 1;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (!mbar_wait(&empty_bar[s], ph)) { timed_out = true; break; }
-                uint8_t *su = smem + (size_t)s * P.stage_bytes, *sv = su + P.u.tile_bytes, *scales = sv + P.v.tile_bytes;
-                const bool with_scales = kb == kb0 || (kb & 3) == 0;
+        // (the whole warp in step, an elected lane issues, as in the pair kernel)
+        uint32_t s = 0, ph = 1, in_group = 0, group = 0;
+        const bool u_k = P.u.major == 0, v_k = P.v.major == 0;
+        for (int kb = kb0; kb < kb1; ++kb) {
+            if (in_group == 0 && !mbar_wait_uniform(&empty_bar[group], ph)) { timed_out = true; break; }
+            if (++in_group == kSplitRelease) { in_group = 0; ++group; }
+            uint8_t *su = smem + (size_t)s * P.stage_bytes, *sv = su + P.u.tile_bytes, *scales = sv + P.v.tile_bytes;
+            const bool with_scales = kb == kb0 || (kb & 3) == 0;
+            const int k0 = kb * 128;
+            if (elect_one()) {
                 mbar_expect_tx(&full_bar[s], P.u.tile_bytes + P.v.tile_bytes + (with_scales ? 2u * kF8Piece : 0u));
-                if (P.u.major == 0) tma_load_2d(su, &P.mapU, &full_bar[s], kb * 128, (int)n0);
-                else                tma_load_2d(su, &P.mapU, &full_bar[s], (int)n0, kb * 128);
-                if (P.v.major == 0) tma_load_2d(sv, &P.mapV, &full_bar[s], kb * 128, (int)m0);
-                else                tma_load_2d(sv, &P.mapV, &full_bar[s], (int)m0, kb * 128);
+                tma_load_2d(su, &P.mapU, &full_bar[s], u_k ? k0 : (int)n0, u_k ? (int)n0 : k0);
+                tma_load_2d(sv, &P.mapV, &full_bar[s], v_k ? k0 : (int)m0, v_k ? (int)m0 : k0);
                 if (with_scales) {
                     tma_load_3d(scales, &P.mapSU, &full_bar[s], 0, kb >> 2, (int)(n0 >> 7));
                     tma_load_3d(scales + kF8Piece, &P.mapSV, &full_bar[s], 0, kb >> 2, (int)(m0 >> 7));
                 }
-                if (++s == (uint32_t)P.stages) { s = 0; ph ^= 1u; }
             }
+            __syncwarp();
+            if (++s == (uint32_t)P.stages) { s = 0; ph ^= 1u; group = 0; }
         }
     } else if (warp == 1) {
-        uint32_t s = 0, ph = 0, set = kSplitSets - 1;
+        uint32_t s = 0, ph = 0, set = kSplitSets - 1, in_group = 0, group = 0;
+        bool ready = false;
         for (int kb = kb0; kb < kb1; ++kb) {
-            if (!mbar_wait_uniform(&full_bar[s], ph)) { timed_out = true; break; }
+            if (!__all_sync(0xffffffffu, ready) && !mbar_wait_uniform(&full_bar[s], ph)) { timed_out = true; break; }
             tc_fence_after();
             const uint32_t su = smem_u32(smem) + s * P.stage_bytes, sv = su + P.u.tile_bytes, scales = sv + P.v.tile_bytes;
+            if (++s == (uint32_t)P.stages) { s = 0; ph ^= 1u; }
+            ready = mbar_test(&full_bar[s], ph);
             if (kb == kb0 || (kb & 3) == 0) {
                 // (this set's last readers, the MMAs of at least 4 (kSplitSets - 1) + 1 blocks ago, are done: the stage of a
                 // later block than theirs has been filled again, at most kSplitMaxStages blocks ago)
@@ -278,31 +309,45 @@ __global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid
             const uint32_t id = (uint32_t)(kb & 3), idesc = P.idesc | (id << 4) | (id << 29);
             const uint32_t t_su = tmem + 128u + 8u * set, t_sv = t_su + 4u;
             const uint32_t u_lo = ((su >> 4) & 0x3FFFu) | P.u.desc_lo, v_lo = ((sv >> 4) & 0x3FFFu) | P.v.desc_lo;
+            if (elect_one()) {
 #pragma unroll
-            for (uint32_t kk = 0; kk < 4; ++kk)
-                if (elect_one())
+                for (uint32_t kk = 0; kk < 4; ++kk)
                     mma_f8(tmem, ((uint64_t)P.u.desc_hi << 32) | (uint64_t)(u_lo + kk * P.u.kstep),
                            ((uint64_t)P.v.desc_hi << 32) | (uint64_t)(v_lo + kk * P.v.kstep), idesc, t_su, t_sv, kb == kb0 && kk == 0 ? 0u : 1u);
-            if (elect_one()) mma_commit(&empty_bar[s]);
-            if (++s == (uint32_t)P.stages) { s = 0; ph ^= 1u; }
+            }
+            if (++in_group == kSplitRelease) {
+                if (elect_one()) mma_commit(&empty_bar[group]);
+                in_group = 0;
+                if (++group * kSplitRelease == (uint32_t)P.stages) group = 0;
+            }
         }
         if (!timed_out && elect_one()) mma_commit(&acc_full);
         __syncwarp();
     }
-    const int quad = warp & 3;
+    // (bn and the parts are powers of two)
+    const int quad = warp & 3, half = (warp - 2) >> 2, log_share = __ffs(P.bn) - __ffs(P.parts), share = 1 << log_share;       // rows that a part adds up
     const int64_t n = n0 + 32 * quad + lane;
-    float *mine = reinterpret_cast<float *>(smem);                 // partial sums [bn][128], where the ring was
+    float *const sums = reinterpret_cast<float *>(smem + (size_t)P.stages * P.stage_bytes) + 32 * quad + lane;                // [parts][share][128]
     if (warp >= 2) {
         if (!mbar_wait_warp(&acc_full, 0)) timed_out = true;
         tc_fence_after();
-        for (int c = 0; c < P.bn && !timed_out; c += 16) {
+    }
+    if (P.parts > 1) { __syncwarp(); cluster_wait(); }
+    if (warp >= 2) {
+        for (int c = 16 * half; c < P.bn && m0 + c < P.M && !timed_out; c += 32) {
             uint32_t r[16];
             tmem_ld_32x16(tmem + ((uint32_t)(32 * quad) << 16) + (uint32_t)c, r);
             tmem_ld_wait();
+            const int rows = (int)min((int64_t)16, P.M - m0 - c);
+            if (P.parts > 1) {
+                const uint32_t mine = smem_u32(sums) + ((uint32_t)part << (9 + log_share));
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                if (P.parts > 1) mine[(c + j) * 128 + 32 * quad + lane] = __uint_as_float(r[j]);
-                else if (n < P.N && m0 + c + j < P.M) split_store(P, (m0 + c + j) * P.N + n, __uint_as_float(r[j]));
+                for (int j = 0; j < 16; ++j)
+                    if (j < rows) store_in_cta(address_in_cta(mine + (uint32_t)(((c + j) & (share - 1)) << 9), (uint32_t)((c + j) >> log_share)), r[j]);
+            } else {
+                if (P.dtype == QBP_F32) split_put<float>(P.out, m0 + c, P.N, n, rows, r);
+                else if (P.dtype == QBP_BF16) split_put<__nv_bfloat16>(P.out, m0 + c, P.N, n, rows, r);
+                else split_put<__half>(P.out, m0 + c, P.N, n, rows, r);
             }
         }
     }
@@ -310,17 +355,16 @@ __global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid
     tc_fence_before();
     __syncthreads();
     if (P.parts > 1) {
-        cluster_barrier();
-        if (warp >= 2 && n < P.N) {
-            const int64_t rows = min((int64_t)P.bn, P.M - m0);
-            for (int64_t j = rows * part / P.parts; j < rows * (part + 1) / P.parts; ++j) {
-                float sum = 0.0f;
-                for (int q = 0; q < P.parts; ++q) sum += load_of_cta(smem_u32(mine + j * 128 + 32 * quad + lane), (uint32_t)q);
-                split_store(P, (m0 + j) * P.N + n, sum);
-            }
+        cluster_arrive();
+        cluster_wait();                                               // every part's sums are here; nobody writes behind this
+        if (warp >= 2) {
+            const int64_t m = m0 + part * share;
+            const int rows = (int)max((int64_t)0, min((int64_t)share, P.M - m));
+            if (P.dtype == QBP_F32) split_add<float>(P.out, m, P.N, n, half, 2, rows, P.parts, share, sums);
+            else if (P.dtype == QBP_BF16) split_add<__nv_bfloat16>(P.out, m, P.N, n, half, 2, rows, P.parts, share, sums);
+            else split_add<__half>(P.out, m, P.N, n, half, 2, rows, P.parts, share, sums);
         }
         __syncwarp();
-        cluster_barrier();                                            // nobody leaves while its partial sums are being read
     }
     if (warp == 1) { __syncwarp(); tmem_dealloc(tmem, kSplitCols); }
 }
@@ -341,6 +385,30 @@ static void launch_clusters(void (*kernel)(P...), dim3 grid, unsigned cluster, u
     (void)cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
+// Clusters of `parts` CTAs that run at the same time, one CTA an SM (a cluster's SMs are of one GPC, whose number is no multiple of
+// eight: of 16 clusters of eight some wait for the others).  Asked once per device.
+static int split_clusters(int parts)
+{
+    static PerDeviceOnce asked[4];
+    static int found[4][kMaxDevices];
+    const int k = parts == 2 ? 1 : parts == 4 ? 2 : 3;
+    int dev = -1;
+    if (asked[k].pending(&dev)) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(parts * 256)); cfg.blockDim = dim3(kSplitThreads); cfg.dynamicSmemBytes = kSplitSmem;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)parts; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr; cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, f8_split_kernel, &cfg) != cudaSuccess) { cudaGetLastError(); n = sm_count() / parts * 3 / 4; }
+        if (dev < 0) return n;
+        found[k][dev] = n;
+        asked[k].mark(dev);
+    }
+    return found[k][dev];
+}
+
 static int launch_f8_split(const F8Product &p, cudaStream_t st)
 {
     F8SplitParams P{};
@@ -356,16 +424,22 @@ static int launch_f8_split(const F8Product &p, cudaStream_t st)
     P.idesc = make_idesc_f8(p.formatB, p.formatA, P.u.major, P.v.major, 128, (uint32_t)P.bn);
     P.k_blocks = (int)f8_blocks(p.K);
     const int64_t tiles_n = f8_blocks(p.N), tiles_m = (p.M + P.bn - 1) / P.bn;
-    P.parts = 1;
-    while (P.parts < kSplitMaxParts && 2 * P.parts * tiles_n * tiles_m <= sm_count() && 4 * P.parts <= P.k_blocks) P.parts *= 2;
-    P.stage_bytes = (uint32_t)align_up(P.u.tile_bytes + P.v.tile_bytes + 2u * kF8Piece, 1024);
-    P.stages = (int)std::min<int64_t>(kSplitMaxStages, (kSplitSmem - 1024) / P.stage_bytes);
-    P.stages = std::min(P.stages, std::max(2, (P.k_blocks + P.parts - 1) / P.parts));
-    static_assert(kSplitMaxStages <= 4 * kSplitSets - 3, "a set of scales is written again while MMAs may read it");
-    const size_t ring = std::max<size_t>((size_t)P.stages * P.stage_bytes, P.parts > 1 ? (size_t)P.bn * 512 : 0);
-    P.M = p.M; P.N = p.N; P.out = p.out; P.dtype = p.dtype; P.status = p.status; P.clear = p.cleared ? 0 : 1;
     static PerDeviceOnce configured;
     QBP_SMEM_OPT_IN(configured, f8_split_kernel, kSplitSmem);
+    // Parts: as many as run at the same time, where they save more blocks of 0.25 us than adding up the tile's rows costs (one call of
+    // many in a row, one part and the best, us: 1 x 4096 x 4096 16.2 and 11.8 (four), 64 x 1024 x 1024 9.6 and 9.0 (eight), 128 x 1024 x
+    // 1024 10.1 and 10.4 (eight), 256 x 4096 x 4096 17.8 and 18.5 (two), x 8192 26.6 and 24.9).
+    P.parts = 1;
+    while (P.parts < kSplitMaxParts && 2 * P.parts <= P.k_blocks && tiles_n * tiles_m <= split_clusters(2 * P.parts)) P.parts *= 2;
+    if (P.k_blocks - (P.k_blocks + P.parts - 1) / P.parts <= 2 + P.bn / 16 * (P.parts == 2 ? 3 : 1)) P.parts = 1;
+    P.stage_bytes = (uint32_t)align_up(P.u.tile_bytes + P.v.tile_bytes + 2u * kF8Piece, 1024);
+    const uint32_t sums_bytes = P.parts > 1 ? (uint32_t)P.bn * 512u : 0u;
+    P.stages = (int)std::min<int64_t>(kSplitMaxStages, (kSplitSmem - 1024 - sums_bytes) / P.stage_bytes);
+    P.stages = std::min(P.stages, std::max(2, (P.k_blocks + P.parts - 1) / P.parts + 1));
+    P.stages -= P.stages % (int)kSplitRelease;
+    static_assert(kSplitMaxStages + (int)kSplitRelease <= 4 * kSplitSets - 3, "a set of scales is written again while MMAs may read it");
+    const size_t ring = (size_t)P.stages * P.stage_bytes + sums_bytes;
+    P.M = p.M; P.N = p.N; P.out = p.out; P.dtype = p.dtype; P.status = p.status; P.clear = p.cleared ? 0 : 1;
     QBP_TRACE_BEGIN(st);
     launch_clusters(f8_split_kernel, dim3((unsigned)(tiles_n * P.parts), (unsigned)tiles_m), (unsigned)P.parts, kSplitThreads, 1024 + ring, st, P);
     QBP_LAUNCH_OK("f8_split_kernel");
@@ -416,7 +490,10 @@ extern "C" __attribute__((visibility("default"))) int qbp_quantize_f8_square(con
 
 static int run_product(const F8Product &p, cudaStream_t st)
 {
-    if (f8_pair_eligible(p)) return launch_f8_pair(p, st);
+    // One wave of tiles of 128 on single CTAs against tiles of 256 rows on pairs (one call of many in a row, split and pair, us): 64 x 4096 x
+    // 8192 15.7 and 27.3, 512 x 4096 x 512 9.9 and 11.5, 1111 x 2048 x 8192 27.6 and 31.0; two waves: 512 x 8192 x 2048 26.3 and 17.4.
+    const int64_t rows = p.transA || p.M > 64 ? 128 : 64;
+    if (f8_blocks(p.N) * ((p.M + rows - 1) / rows) > sm_count()) return launch_f8_pair(p, st);
     return launch_f8_split(p, st);
 }
 

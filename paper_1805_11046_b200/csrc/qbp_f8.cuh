@@ -39,7 +39,6 @@ struct F8Product {
     void *out; int dtype;
     int *status; bool cleared;                                    // whether the status word is zero already
 };
-bool f8_pair_eligible(const F8Product &p);
 int launch_f8_pair(const F8Product &p, cudaStream_t st);
 
 #ifdef __CUDACC__
@@ -88,6 +87,19 @@ __device__ __forceinline__ void tma_load_3d(void *dst, const void *map, uint64_t
         "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
         ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
         : "memory");
+}
+// Whether the barrier's phase is complete, without waiting (try_wait may hold the thread for microseconds where it is not).
+__device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
 }
 // Descriptor of a piece of scales in shared memory (no swizzle, groups of 8 rows of 16 bytes 128 bytes apart).
 __device__ __forceinline__ uint64_t piece_desc(uint32_t smem_addr)

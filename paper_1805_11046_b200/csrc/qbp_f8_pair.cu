@@ -98,7 +98,7 @@ __device__ __forceinline__ bool fp_mma_loop(const FpMmaArgs &A)
             const uint32_t here = at;
             at += A.stage_bytes;
             if (++s == A.stages) { s = 0; ph ^= 1u; at = A.ring; }
-            ready = mbar_try_wait(&A.full_bar[s], ph);
+            ready = mbar_test(&A.full_bar[s], ph);
             if ((kb & 3) == 0) {
                 set = set + 1 == A.sets ? 0u : set + 1;
                 t_sa = A.tmem + A.set_col + set * A.set_cols;
@@ -111,11 +111,12 @@ __device__ __forceinline__ bool fp_mma_loop(const FpMmaArgs &A)
             }
             const uint32_t id = (uint32_t)(kb & 3), idesc = A.idesc | (id << 4) | (id << 29);
             const uint32_t a_lo = ((here >> 4) & 0x3FFFu) | A.a_desc_lo, b_lo = (((here + A.a_bytes) >> 4) & 0x3FFFu) | A.b_desc_lo;
+            if (elect_one()) {
 #pragma unroll
-            for (uint32_t kk = 0; kk < 4; ++kk)
-                if (elect_one())
+                for (uint32_t kk = 0; kk < 4; ++kk)
                     mma_f8_pair(d_tmem, ((uint64_t)a_hi << 32) | (uint64_t)(a_lo + kk * AK), ((uint64_t)b_hi << 32) | (uint64_t)(b_lo + kk * BK),
                                 idesc, t_sa, t_sa + 4u, kk == 0 && kb == 0 ? 0u : 1u);
+            }
             if (++in_group == kFpRelease) {
                 if (elect_one()) mma_commit_pair(&A.empty_bar[group]);
                 in_group = 0;
@@ -309,18 +310,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFpThreads, 1) f8_pa
     if (warp == 1) { __syncwarp(); tmem_dealloc_pair(tmem_base, 512); }
 }
 
-bool f8_pair_eligible(const F8Product &p)
-{
-    return p.M >= 256 && p.N >= 128;
-}
-
 int launch_f8_pair(const F8Product &p, cudaStream_t st)
 {
     F8PairParams P{};
     int rc;
     const auto tiles_of = [&](int64_t n) { return ((p.M + 255) / 256) * ((p.N + n - 1) / n); };
     const int pairs = sm_count() / 2;
-    P.bn = tiles_of(256) > pairs ? 256 : 128;
+    // tiles of 128 columns where they fit the pairs once: their epilogues and first stages are shorter (256 x 2048 x 8192 30.7 us, of 256
+    // columns 34.8); in a second round they are slower (2048 x 2048 x 8192 53.2 and 38.9)
+    P.bn = tiles_of(128) > pairs ? 256 : 128;
     const uint32_t half = (uint32_t)P.bn / 2;
     if (!p.transA) { P.a = layout_kmajor(128, 128);         rc = make_map_2d(&P.mapA, p.A, p.M, p.K, 128, 128); }
     else           { P.a = layout_mnmajor(128, 128, 1, 0);  rc = make_map_2d(&P.mapA, p.A, p.K, p.M, 128, 128); }
