@@ -458,22 +458,41 @@ def _dtype(t) -> int:
         raise TypeError(f"{t}: fp32, bf16 or fp16 is wanted") from None
 
 
+_current_device = torch._C._cuda_getDevice          # (torch.cuda.current_device() without its check for a first use, which every tensor has had)
+_EMPTY = {}
+
+
 def _here(*tensors) -> int:
     """The current device's index; every tensor given has to be on it (work is enqueued on its current stream)."""
-    index = torch.cuda.current_device()
+    index = _current_device()
     for t in tensors:
         if t is not None and t.get_device() != index:
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{index}")
     return index
 
 
+def _new(shape, dtype, index):
+    """An uncleared tensor on a device, made from an empty one of its type: without arguments for type and device the allocation
+    takes 1.4 us of the host's time instead of 2.4."""
+    t = _EMPTY.get((dtype, index))
+    if t is None: t = _EMPTY[dtype, index] = torch.empty(0, dtype=dtype, device=torch.device("cuda", index))
+    return t.new_empty(shape)
+
+
+def _scratch(nbytes, index):
+    """workspace() of the current stream, its usual case first."""
+    t = _workspaces.by_stream.get((index, _stream_handle(index)))
+    return t if t is not None and t.numel() >= nbytes else workspace(nbytes, torch.device("cuda", index))
+
+
 def _rows_of(x):
     """x as a matrix: (rows, columns, elements between rows).  Two dimensions may have padded rows, more have to be dense."""
     if x.dim() == 2:
         rows, cols = x.shape
+        if x.is_contiguous(): return rows, cols, cols
         if cols > 1 and x.stride(1) != 1:
             raise ValueError("the innermost dimension has to be dense")
-        return rows, cols, x.stride(0) if rows > 1 else max(cols, 1)
+        return rows, cols, x.stride(0) if rows > 1 else cols
     if not x.is_contiguous():
         raise ValueError("a tensor of other than two dimensions has to be contiguous")
     cols = x.shape[-1] if x.dim() else 1
@@ -493,6 +512,11 @@ def _codes(t):
     return _addr(t)
 
 
+def _scale_bytes(outer, reduction):
+    """qbp_f8_scale_bytes"""
+    return (outer + 127) // 128 * ((reduction + 511) // 512) * 512
+
+
 def qbp_f8_scales(outer: int, reduction: int, device="cuda") -> torch.Tensor:
     """Storage for the scales of an operand of `outer` rows (or columns) and `reduction` reduction indices."""
     return torch.empty(lib.qbp_f8_scale_bytes(outer, reduction), dtype=torch.uint8, device=device)
@@ -510,11 +534,14 @@ def qbp_quantize_f8(x, format=QBP_E4M3, rows=True, cols=False):
     both from one read: (q_rows, s_rows, q_cols, s_cols).  x: [..., columns], fp32, bf16 or fp16."""
     device = _here(x)
     r, c, ld = _rows_of(x)
-    qr = sr = qc = sc = None
-    if rows: qr, sr = torch.empty(x.shape, dtype=torch.uint8, device=x.device), qbp_f8_scales(r, c, x.device)
-    if cols: qc, sc = torch.empty(x.shape, dtype=torch.uint8, device=x.device), qbp_f8_scales(c, r, x.device)
-    _check(lib.qbp_quantize_f8(x.data_ptr(), _dtype(x.dtype), r, c, ld, format, qr.data_ptr() if rows else None, sr.data_ptr() if rows else None,
-                               qc.data_ptr() if cols else None, sc.data_ptr() if cols else None, _stream_handle(device)))
+    qr = sr = qc = sc = p0 = p1 = p2 = p3 = None
+    if rows:
+        qr, sr = _new(x.shape, torch.uint8, device), _new(_scale_bytes(r, c), torch.uint8, device)
+        p0, p1 = qr.data_ptr(), sr.data_ptr()
+    if cols:
+        qc, sc = _new(x.shape, torch.uint8, device), _new(_scale_bytes(c, r), torch.uint8, device)
+        p2, p3 = qc.data_ptr(), sc.data_ptr()
+    _check(lib.qbp_quantize_f8(x.data_ptr(), _dtype(x.dtype), r, c, ld, format, p0, p1, p2, p3, _stream_handle(device)))
     return (qr, sr, qc, sc) if rows and cols else (qr, sr) if rows else (qc, sc)
 
 
@@ -523,15 +550,15 @@ def qbp_quantize_f8_square(x, format=QBP_E4M3):
     columns and over the rows: (q, s_rows, s_cols)."""
     device = _here(x)
     r, c, ld = _rows_of(x)
-    q, sr, sc = torch.empty(x.shape, dtype=torch.uint8, device=x.device), qbp_f8_scales(r, c, x.device), qbp_f8_scales(c, r, x.device)
+    q, sr, sc = _new(x.shape, torch.uint8, device), _new(_scale_bytes(r, c), torch.uint8, device), _new(_scale_bytes(c, r), torch.uint8, device)
     _check(lib.qbp_quantize_f8_square(x.data_ptr(), _dtype(x.dtype), r, c, ld, format, q.data_ptr(), sr.data_ptr(), sc.data_ptr(),
                                       _stream_handle(device)))
     return q, sr, sc
 
 
 def _scales_fit(s, outer, reduction, name):
-    if s.numel() != lib.qbp_f8_scale_bytes(outer, reduction):
-        raise ValueError(f"{name}: {s.numel()} bytes, scales of {outer} x {reduction} are {lib.qbp_f8_scale_bytes(outer, reduction)}")
+    if s.numel() != _scale_bytes(outer, reduction):
+        raise ValueError(f"{name}: {s.numel()} bytes, scales of {outer} x {reduction} are {_scale_bytes(outer, reduction)}")
 
 
 def qbp_gemm_f8(A, sA, B, sB, transA=False, transB=False, formatA=QBP_E4M3, formatB=QBP_E4M3, out_dtype=torch.float32, out=None, ws=None):
@@ -543,9 +570,9 @@ def qbp_gemm_f8(A, sA, B, sB, transA=False, transB=False, formatA=QBP_E4M3, form
     N, kb = B.shape if transB else B.shape[::-1]
     if kb != K: raise ValueError(f"the reduction is {K} in A and {kb} in B")
     _scales_fit(sA, M, K, "sA"); _scales_fit(sB, N, K, "sB")
-    if out is None: out = torch.empty((M, N), dtype=out_dtype, device=A.device)
+    if out is None: out = _new((M, N), out_dtype, device)
     elif tuple(out.shape) != (M, N): raise ValueError(f"out is {tuple(out.shape)}, the product {(M, N)}")
-    if ws is None: ws = workspace(256, A.device)
+    if ws is None: ws = _scratch(256, device)
     _check(lib.qbp_gemm_f8(int(transA), int(transB), M, N, K, formatA, _codes(A), _codes(sA), formatB, _codes(B), _codes(sB), _dtype(out.dtype),
                            _addr(out), ws.data_ptr(), ws.numel(), _stream_handle(device)))
     return out
@@ -558,9 +585,9 @@ def qbp_linear_f8(x, w, sw, w_format=QBP_E4M3, y=None, ws=None):
     N, kw = w.shape
     if kw != K: raise ValueError(f"x has {K} columns, w {kw}")
     _scales_fit(sw, N, K, "sw")
-    if y is None: y = torch.empty((*x.shape[:-1], N), dtype=x.dtype, device=x.device)
+    if y is None: y = _new((*x.shape[:-1], N), x.dtype, device)
     elif tuple(y.shape) != (*x.shape[:-1], N) or y.dtype != x.dtype: raise ValueError(f"y is {tuple(y.shape)} {y.dtype}, the output {(*x.shape[:-1], N)} {x.dtype}")
-    if ws is None: ws = workspace(lib.qbp_linear_f8_workspace_bytes(M, N, K), x.device)
+    if ws is None: ws = _scratch(lib.qbp_linear_f8_workspace_bytes(M, N, K), device)
     _check(lib.qbp_linear_f8(x.data_ptr(), _dtype(x.dtype), ld, M, N, K, w_format, _codes(w), _codes(sw), _addr(y), ws.data_ptr(), ws.numel(),
                              _stream_handle(device)))
     return y
@@ -595,16 +622,17 @@ def qbp_resnorm_fwd(d: ResnormDesc, x, b=None, w_post=None, gate=None, w_pre=Non
     """Returns (r, h, rstd_post, rstd_pre), None where there is none: r without a block output and alpha 1 is x itself, h and its
     rstd without a norm before the next block.  h has b's type (without b, x's)."""
     device = _here(x, b, w_post, gate, w_pre, r, h, rstd_post, rstd_pre)
-    n, e = d.rows * d.cols, torch.empty
+    rows, cols, xt, bt = d.rows, d.cols, d.x_dtype, d.b_dtype
+    n = rows * cols
     if r is None and not (b is None and d.alpha == 1.0): r = torch.empty_like(x)
     if d.pre:
         if h is None: h = torch.empty_like(x if b is None else b)
-        if rstd_pre is None: rstd_pre = e(d.rows, dtype=torch.float32, device=x.device)
-    if d.post and rstd_post is None: rstd_post = e(d.rows, dtype=torch.float32, device=x.device)
-    _check(lib.qbp_resnorm_fwd(C.addressof(d), _real(x, n, d.x_dtype, "x"), _real(b, n, d.b_dtype, "b"), _real(w_post, d.cols, QBP_F32, "w_post"),
-                               _real(gate, _gates(d) * d.cols, QBP_F32, "gate"), _real(w_pre, d.cols, QBP_F32, "w_pre"),
-                               _real(r, n, d.x_dtype, "r"), _real(h, n, d.b_dtype, "h"), _real(rstd_post, d.rows, QBP_F32, "rstd_post"),
-                               _real(rstd_pre, d.rows, QBP_F32, "rstd_pre"), _stream_handle(device)))
+        if rstd_pre is None: rstd_pre = _new(rows, torch.float32, device)
+    if d.post and rstd_post is None: rstd_post = _new(rows, torch.float32, device)
+    _check(lib.qbp_resnorm_fwd(C.addressof(d), _real(x, n, xt, "x"), _real(b, n, bt, "b"), _real(w_post, cols, QBP_F32, "w_post"),
+                               _real(gate, _gates(d) * cols, QBP_F32, "gate"), _real(w_pre, cols, QBP_F32, "w_pre"),
+                               _real(r, n, xt, "r"), _real(h, n, bt, "h"), _real(rstd_post, rows, QBP_F32, "rstd_post"),
+                               _real(rstd_pre, rows, QBP_F32, "rstd_pre"), _stream_handle(device)))
     return r, h, rstd_post, rstd_pre
 
 
@@ -613,18 +641,18 @@ def qbp_resnorm_bwd(d: ResnormDesc, dr, dh, b, r, rstd_post, rstd_pre, w_post=No
     """The gradients (dx, db, dw_post, dgate, dw_pre) from dr (None: nothing else uses r) and dh.  Gradients of what the forward
     did not have are None; want_params=False: dx and db alone."""
     device = _here(dr, dh, b, r, rstd_post, rstd_pre, w_post, gate, w_pre, dx, db, ws)
-    n, like = d.rows * d.cols, dr if dr is not None else r
+    rows, cols, xt, bt = d.rows, d.cols, d.x_dtype, d.b_dtype
+    n, like = rows * cols, dr if dr is not None else r
     if dx is None: dx = torch.empty_like(like)
     if db is None and b is not None: db = torch.empty_like(b)
-    f32 = lambda *shape: torch.empty(shape, dtype=torch.float32, device=like.device)
-    dw1 = f32(d.cols) if want_params and d.post else None
-    dg = f32(_gates(d), d.cols) if want_params and gate is not None else None
-    dw2 = f32(d.cols) if want_params and d.pre else None
-    if ws is None: ws = workspace(lib.qbp_resnorm_bwd_workspace_bytes(C.addressof(d)), like.device)
-    _check(lib.qbp_resnorm_bwd(C.addressof(d), _real(dr, n, d.x_dtype, "dr"), _real(dh, n, d.b_dtype, "dh"), _real(b, n, d.b_dtype, "b"),
-                               _real(r, n, d.x_dtype, "r"), _real(rstd_post, d.rows, QBP_F32, "rstd_post"), _real(rstd_pre, d.rows, QBP_F32, "rstd_pre"),
-                               _real(w_post, d.cols, QBP_F32, "w_post"), _real(gate, _gates(d) * d.cols, QBP_F32, "gate"),
-                               _real(w_pre, d.cols, QBP_F32, "w_pre"), _real(dx, n, d.x_dtype, "dx"), _real(db, n, d.b_dtype, "db"),
+    dw1 = _new(cols, torch.float32, device) if want_params and d.post else None
+    dg = _new((_gates(d), cols), torch.float32, device) if want_params and gate is not None else None
+    dw2 = _new(cols, torch.float32, device) if want_params and d.pre else None
+    if ws is None: ws = _scratch(lib.qbp_resnorm_bwd_workspace_bytes(C.addressof(d)), device)
+    _check(lib.qbp_resnorm_bwd(C.addressof(d), _real(dr, n, xt, "dr"), _real(dh, n, bt, "dh"), _real(b, n, bt, "b"),
+                               _real(r, n, xt, "r"), _real(rstd_post, rows, QBP_F32, "rstd_post"), _real(rstd_pre, rows, QBP_F32, "rstd_pre"),
+                               _real(w_post, cols, QBP_F32, "w_post"), _real(gate, _gates(d) * cols, QBP_F32, "gate"),
+                               _real(w_pre, cols, QBP_F32, "w_pre"), _real(dx, n, xt, "dx"), _real(db, n, bt, "db"),
                                _addr(dw1), _addr(dg), _addr(dw2), ws.data_ptr(), ws.numel(), _stream_handle(device)))
     return dx, db, dw1, dg, dw2
 

@@ -74,5 +74,18 @@ template <typename T> __device__ __forceinline__ void store8(T *p, const Raw8<T>
     }
 }
 
+// 32 bytes at a time, on a 32-byte boundary: eight fp32 of a lane in one access.  (As two of 16 bytes each access asks for half of 32
+// sectors.)
+__device__ __forceinline__ void put32(void *p, const uint4 &a, const uint4 &b)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+                 : "memory");
+}
+__device__ __forceinline__ void get32(const void *p, uint4 &a, uint4 &b)
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p) : "memory");
+}
+
 #endif  // __CUDACC__
 }  // namespace qbp

@@ -214,11 +214,6 @@ template <typename T> __device__ __forceinline__ void ring_read(const uint4 *slo
     for (int i = 0; i < Pieces<T>::n; ++i) r.w[i] = slot[i];
     unpack8(r, v);
 }
-__device__ __forceinline__ void put32(void *p, const uint4 &a, const uint4 &b)
-{
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
-                 : "memory");
-}
 // (wide: fp32 rows start on 32-byte boundaries)
 template <typename T> __device__ __forceinline__ void put_vec(void *row0, int64_t at, const Raw8<T> &r, int wide)
 {
