@@ -449,6 +449,7 @@ def qbp_gated_xnor_gemm_bits(nz_bits, sign_bits, B_bits, K, out=None):
 
 # ------------------------------------------- 8-bit floating point with a scale for each block of 128
 _DTYPES = {torch.float32: QBP_F32, torch.bfloat16: QBP_BF16, torch.float16: QBP_F16}
+_REALS = tuple(_DTYPES)                              # by qbp_dtype
 
 
 def _dtype(t) -> int:
@@ -597,12 +598,13 @@ def qbp_linear_f8(x, w, sw, w_format=QBP_E4M3, y=None, ws=None):
 QBP_RESNORM_MAX_COLS = 16384
 
 
-def resnorm_desc(x, b=None, alpha=1.0, eps=1e-6, gate_rows=0, p=0.0, seed=0, tensor_id=0, index_base=0, post=None, pre=True) -> ResnormDesc:
+def resnorm_desc(x, b=None, alpha=1.0, eps=1e-6, gate_rows=0, p=0.0, seed=0, tensor_id=0, index_base=0, post=None, pre=True, h_dtype=None) -> ResnormDesc:
     """The join of the residual stream x [..., columns] with a block's output b: r = alpha x + gate * dropout(norm(b) w_post),
     h = norm(r) w_pre.  post / pre: whether there is a norm after the block (by default with b) and before the next one;
-    gate_rows: rows that share a row of the gate (0: all); p, seed, tensor_id, index_base: the dropout's, as in qbp_dropout."""
+    gate_rows: rows that share a row of the gate (0: all); p, seed, tensor_id, index_base: the dropout's, as in qbp_dropout.
+    h_dtype: of the norm before a first block (no b), the type of h where it is not x's."""
     cols = x.shape[-1]
-    return ResnormDesc(x.numel() // cols if cols else 0, cols, _dtype(x.dtype), _dtype((x if b is None else b).dtype), int(b is not None if post is None else post),
+    return ResnormDesc(x.numel() // cols if cols else 0, cols, _dtype(x.dtype), _dtype(b.dtype if b is not None else h_dtype or x.dtype), int(b is not None if post is None else post),
                        int(pre), eps, alpha, gate_rows, p, tensor_id, seed, index_base)
 
 
@@ -620,13 +622,13 @@ def _gates(d) -> int:
 
 def qbp_resnorm_fwd(d: ResnormDesc, x, b=None, w_post=None, gate=None, w_pre=None, r=None, h=None, rstd_post=None, rstd_pre=None):
     """Returns (r, h, rstd_post, rstd_pre), None where there is none: r without a block output and alpha 1 is x itself, h and its
-    rstd without a norm before the next block.  h has b's type (without b, x's)."""
+    rstd without a norm before the next block.  h has b's type (without b, the descriptor's)."""
     device = _here(x, b, w_post, gate, w_pre, r, h, rstd_post, rstd_pre)
     rows, cols, xt, bt = d.rows, d.cols, d.x_dtype, d.b_dtype
     n = rows * cols
     if r is None and not (b is None and d.alpha == 1.0): r = torch.empty_like(x)
     if d.pre:
-        if h is None: h = torch.empty_like(x if b is None else b)
+        if h is None: h = torch.empty_like(b) if b is not None else _new(x.shape, _REALS[bt], device)
         if rstd_pre is None: rstd_pre = _new(rows, torch.float32, device)
     if d.post and rstd_post is None: rstd_post = _new(rows, torch.float32, device)
     _check(lib.qbp_resnorm_fwd(C.addressof(d), _real(x, n, xt, "x"), _real(b, n, bt, "b"), _real(w_post, cols, QBP_F32, "w_post"),

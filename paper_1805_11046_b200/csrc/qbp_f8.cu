@@ -152,7 +152,6 @@ static void launch_f8_quantize_as(const T *x, int64_t rows, int64_t cols, int64_
 static int launch_f8_quantize(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int format, int what, uint8_t *q_rows,
                               uint8_t *s_rows, uint8_t *q_cols, uint8_t *s_cols, cudaStream_t st)
 {
-    if (rows == 0 || cols == 0) return QBP_OK;
     QBP_TRACE_BEGIN(st);
     if (format == QBP_E4M3) QBP_FOR_DTYPE(dtype, T, (launch_f8_quantize_as<T, QBP_E4M3>((const T *)x, rows, cols, ld, what, q_rows, s_rows, q_cols, s_cols, st)));
     else                    QBP_FOR_DTYPE(dtype, T, (launch_f8_quantize_as<T, QBP_E5M2>((const T *)x, rows, cols, ld, what, q_rows, s_rows, q_cols, s_cols, st)));
@@ -169,17 +168,26 @@ static int launch_f8_quantize(const void *x, int dtype, int64_t rows, int64_t co
 // sums of these rows into its shared memory (reading them there took a round trip a row: 128 x 1024 x 512 22.6 us with the launch).
 //
 // Roles: warp 0 loads by TMA, warp 1 copies scales to tensor memory and issues the MMAs, warps 2..9 take the accumulator out.
+// Of a layer that serves few rows (TX: their type), warps 2..9 first quantise the rows, each CTA its part of the reduction, straight into
+// the stages, with the scales of one block at a time.
 // Every wait is bounded.
 constexpr int kSplitThreads = 320;
 constexpr int kSplitMaxStages = 10;
 constexpr uint32_t kSplitRelease = 2;            // stages released by one commit
 constexpr int kSplitMaxParts = 8;
 constexpr uint32_t kSplitSmem = 220u * 1024u;
-constexpr uint32_t kSplitCols = 256;             // tensor memory: the accumulator in [0, 128), then four sets of 8 columns of scales
-constexpr int kSplitSets = 4;
+constexpr uint32_t kSplitCols = 256;             // tensor memory: the accumulator in [0, 128), then sets of 4 columns of scales:
+constexpr uint32_t kSplitSetU = 128, kSplitSetV = 144;
+constexpr int kSplitSets = 4, kSplitBlockSets = 16;      // of U (and of V from memory), a set for four blocks; of V quantised here, for one
+constexpr int64_t kSplitQuantise = 16;
+constexpr int kSplitDeclined = 1;                // launch_f8_split: too many rows to quantise on the way
+constexpr int kSplitAhead = 8;                   // pairs of rows that a quantising warp loads ahead
 
 struct F8SplitParams {
-    CUtensorMap mapU, mapV, mapSU, mapSV;        // U: the output's columns (operand B), V: its rows (operand A)
+    CUtensorMap mapU, mapV;                      // U: the output's columns (operand B), V: its rows (operand A)
+    const uint8_t *su, *sv;                      // their scales
+    int64_t groups;                              // pieces of scales along the reduction
+    const void *x; int64_t ld, K; int vec;       // the rows as real numbers, quantised here (no mapV, no sv)
     OperandLayout u, v;
     uint32_t idesc, stage_bytes;
     int bn, stages, k_blocks, parts, clear;
@@ -235,8 +243,65 @@ template <typename T> __device__ __forceinline__ void split_add(void *out, int64
     }
 }
 
+// Warps 2..9: the blocks kb0..kb1 of all rows (at most bn) to e4m3, into the stages as the product wants them: rows of 128 bytes,
+// 16-byte pieces swizzled by the row, and each row's scale byte at its place in a piece.  Every eighth block is a warp's (with all warps on
+// one block, one block after the other, a block took half a microsecond, nearly all of it latency), two rows at a time, sixteen lanes to a
+// row, the next rows' loads on their way.  False when a wait ran out.
+template <typename T>
+__device__ __forceinline__ bool split_quantise(const F8SplitParams &P, uint8_t *smem, uint64_t *full_bar, uint64_t *empty_bar, int kb0, int kb1)
+{
+    const int lane = threadIdx.x & 31, lane16 = lane & 15, high = lane >> 4;
+    const int M = (int)P.M, first = kb0 + (int)(threadIdx.x >> 5) - 2;
+    uint32_t s = (uint32_t)(first - kb0), ph = 1;
+    while (s >= (uint32_t)P.stages) { s -= (uint32_t)P.stages; ph ^= 1u; }
+    for (int kb = first; kb < kb1; kb += 8) {
+        const int64_t c = 128ll * kb + 8 * lane16;
+        const T *x = static_cast<const T *>(P.x) + (c < P.K ? c : 0);
+        const auto load = [&](int r) { return load8(x + (r < M ? r : 0) * P.ld, r < M && c < P.K ? 8 : 0, P.vec != 0); };
+        Raw8<T> ahead[kSplitAhead];
+#pragma unroll
+        for (int a = 0; a < kSplitAhead; ++a) ahead[a] = load(2 * a + high);
+        if (!mbar_wait_warp(&empty_bar[s / kSplitRelease], ph)) return false;
+        uint8_t *const sv = smem + (size_t)s * P.stage_bytes + P.u.tile_bytes, *const bytes = sv + P.v.tile_bytes + kF8Piece + (kb & 3);
+        for (int r0 = high; r0 - high < M; r0 += 2 * kSplitAhead) {
+#pragma unroll
+            for (int a = 0; a < kSplitAhead; ++a) {
+                const int r = r0 + 2 * a;
+                if (r - high >= M) break;
+                float v[8];
+                unpack8(ahead[a], v);
+                if (r - high + 2 * kSplitAhead < M) ahead[a] = load(r + 2 * kSplitAhead);
+                float m = amax3(amax3(amax3(amax3(v[0], v[1], v[2]), v[3], v[4]), v[5], v[6]), v[7], 0.0f);
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) m = amax3(m, __shfl_xor_sync(0xFFFFFFFFu, m, o), 0.0f);
+                const uint32_t byte = f8_scale_byte<QBP_E4M3>(m);
+                const float inv = f8_inverse(byte);
+                if (r < M) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], inv);
+                    *reinterpret_cast<uint2 *>(sv + r * 128 + (((lane16 >> 1) ^ (r & 7)) << 4) + (lane16 & 1) * 8) = f8_codes8<QBP_E4M3>(v);
+                    if (lane16 == 0) bytes[(r & 31) * 16 + (r >> 5) * 4] = (uint8_t)byte;
+                }
+            }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full_bar[s]);
+        s += 8u;
+        while (s >= (uint32_t)P.stages) { s -= (uint32_t)P.stages; ph ^= 1u; }
+    }
+    return true;
+}
+
+struct FromCodes {};
+template <typename TX> struct SplitRows { static constexpr bool quantise = true; using type = TX; };
+template <> struct SplitRows<FromCodes> { static constexpr bool quantise = false; using type = float; };
+
+template <typename TX>
 __global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid_constant__ F8SplitParams P)
 {
+    constexpr bool kQuantise = SplitRows<TX>::quantise;
+    using T = typename SplitRows<TX>::type;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full_bar[kSplitMaxStages], empty_bar[kSplitMaxStages / kSplitRelease], acc_full;
     __shared__ uint32_t tmem_slot;
@@ -248,11 +313,12 @@ __global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid
     const int kb0 = (int)((int64_t)P.k_blocks * part / P.parts), kb1 = (int)((int64_t)P.k_blocks * (part + 1) / P.parts);
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < P.stages; ++s) mbar_init(&full_bar[s], 1);
+        for (int s = 0; s < P.stages; ++s) mbar_init(&full_bar[s], kQuantise ? 2 : 1);
         for (int g = 0; g < P.stages / (int)kSplitRelease; ++g) mbar_init(&empty_bar[g], 1);
         mbar_init(&acc_full, 1);
         mbar_fence_init();
-        tma_prefetch_desc(&P.mapU); tma_prefetch_desc(&P.mapV); tma_prefetch_desc(&P.mapSU); tma_prefetch_desc(&P.mapSV);
+        tma_prefetch_desc(&P.mapU);
+        if (!kQuantise) tma_prefetch_desc(&P.mapV);
     }
     if (warp == 1) { tmem_alloc(&tmem_slot, kSplitCols); tmem_relinquish(); }
     tc_fence_before();
@@ -277,19 +343,19 @@ __global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid
             const bool with_scales = kb == kb0 || (kb & 3) == 0;
             const int k0 = kb * 128;
             if (elect_one()) {
-                mbar_expect_tx(&full_bar[s], P.u.tile_bytes + P.v.tile_bytes + (with_scales ? 2u * kF8Piece : 0u));
+                mbar_expect_tx(&full_bar[s], P.u.tile_bytes + (kQuantise ? 0u : P.v.tile_bytes) + (with_scales ? (kQuantise ? 1u : 2u) * kF8Piece : 0u));
                 tma_load_2d(su, &P.mapU, &full_bar[s], u_k ? k0 : (int)n0, u_k ? (int)n0 : k0);
-                tma_load_2d(sv, &P.mapV, &full_bar[s], v_k ? k0 : (int)m0, v_k ? (int)m0 : k0);
+                if (!kQuantise) tma_load_2d(sv, &P.mapV, &full_bar[s], v_k ? k0 : (int)m0, v_k ? (int)m0 : k0);
                 if (with_scales) {
-                    tma_load_3d(scales, &P.mapSU, &full_bar[s], 0, kb >> 2, (int)(n0 >> 7));
-                    tma_load_3d(scales + kF8Piece, &P.mapSV, &full_bar[s], 0, kb >> 2, (int)(m0 >> 7));
+                    bulk_load(scales, P.su + ((n0 >> 7) * P.groups + (kb >> 2)) * kF8Piece, kF8Piece, &full_bar[s]);
+                    if (!kQuantise) bulk_load(scales + kF8Piece, P.sv + ((m0 >> 7) * P.groups + (kb >> 2)) * kF8Piece, kF8Piece, &full_bar[s]);
                 }
             }
             __syncwarp();
             if (++s == (uint32_t)P.stages) { s = 0; ph ^= 1u; group = 0; }
         }
     } else if (warp == 1) {
-        uint32_t s = 0, ph = 0, set = kSplitSets - 1, in_group = 0, group = 0;
+        uint32_t s = 0, ph = 0, set = kSplitSets - 1, vset = kSplitBlockSets - 1, in_group = 0, group = 0;
         bool ready = false;
         for (int kb = kb0; kb < kb1; ++kb) {
             if (!__all_sync(0xffffffffu, ready) && !mbar_wait_uniform(&full_bar[s], ph)) { timed_out = true; break; }
@@ -297,17 +363,17 @@ __global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid
             const uint32_t su = smem_u32(smem) + s * P.stage_bytes, sv = su + P.u.tile_bytes, scales = sv + P.v.tile_bytes;
             if (++s == (uint32_t)P.stages) { s = 0; ph ^= 1u; }
             ready = mbar_test(&full_bar[s], ph);
-            if (kb == kb0 || (kb & 3) == 0) {
-                // (this set's last readers, the MMAs of at least 4 (kSplitSets - 1) + 1 blocks ago, are done: the stage of a
-                // later block than theirs has been filled again, at most kSplitMaxStages blocks ago)
-                set = set + 1 == kSplitSets ? 0u : set + 1;
-                if (elect_one()) {
-                    copy_piece(tmem + 128u + 8u * set, piece_desc(scales));
-                    copy_piece(tmem + 128u + 8u * set + 4u, piece_desc(scales + kF8Piece));
-                }
+            // (a set's last readers, the MMAs of at least 4 (kSplitSets - 1) + 1 blocks ago, or kSplitBlockSets, are done: the stage of a
+            // later block than theirs has been filled again, at most kSplitMaxStages + kSplitRelease blocks ago)
+            const bool with_scales = kb == kb0 || (kb & 3) == 0;
+            if (with_scales) set = set + 1 == kSplitSets ? 0u : set + 1;
+            if (kQuantise) vset = vset + 1 == kSplitBlockSets ? 0u : vset + 1;
+            const uint32_t t_su = tmem + kSplitSetU + 4u * set, t_sv = tmem + kSplitSetV + 4u * (kQuantise ? vset : set);
+            if ((kQuantise || with_scales) && elect_one()) {
+                if (with_scales) copy_piece(t_su, piece_desc(scales));
+                copy_piece(t_sv, piece_desc(scales + kF8Piece));
             }
             const uint32_t id = (uint32_t)(kb & 3), idesc = P.idesc | (id << 4) | (id << 29);
-            const uint32_t t_su = tmem + 128u + 8u * set, t_sv = t_su + 4u;
             const uint32_t u_lo = ((su >> 4) & 0x3FFFu) | P.u.desc_lo, v_lo = ((sv >> 4) & 0x3FFFu) | P.v.desc_lo;
             if (elect_one()) {
 #pragma unroll
@@ -329,7 +395,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid
     const int64_t n = n0 + 32 * quad + lane;
     float *const sums = reinterpret_cast<float *>(smem + (size_t)P.stages * P.stage_bytes) + 32 * quad + lane;                // [parts][share][128]
     if (warp >= 2) {
-        if (!mbar_wait_warp(&acc_full, 0)) timed_out = true;
+        if (kQuantise) timed_out = !split_quantise<T>(P, smem, full_bar, empty_bar, kb0, kb1);
+        if (!timed_out && !mbar_wait_warp(&acc_full, 0)) timed_out = true;
         tc_fence_after();
     }
     if (P.parts > 1) { __syncwarp(); cluster_wait(); }
@@ -401,7 +468,7 @@ static int split_clusters(int parts)
         attr.val.clusterDim.x = (unsigned)parts; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
         cfg.attrs = &attr; cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, f8_split_kernel, &cfg) != cudaSuccess) { cudaGetLastError(); n = sm_count() / parts * 3 / 4; }
+        if (cudaOccupancyMaxActiveClusters(&n, f8_split_kernel<FromCodes>, &cfg) != cudaSuccess) { cudaGetLastError(); n = sm_count() / parts * 3 / 4; }
         if (dev < 0) return n;
         found[k][dev] = n;
         asked[k].mark(dev);
@@ -409,7 +476,10 @@ static int split_clusters(int parts)
     return found[k][dev];
 }
 
-static int launch_f8_split(const F8Product &p, cudaStream_t st)
+// Rows as real numbers, to be quantised on the way (x NULL: codes and scales are there).
+struct SplitInput { const void *x; int64_t ld; };
+
+static int launch_f8_split(const F8Product &p, const SplitInput &in, cudaStream_t st)
 {
     F8SplitParams P{};
     int rc;
@@ -417,18 +487,16 @@ static int launch_f8_split(const F8Product &p, cudaStream_t st)
     if (p.transB) { P.u = layout_kmajor(128, 128);        rc = make_map_2d(&P.mapU, p.B, p.N, p.K, 128, 128); }
     else          { P.u = layout_mnmajor(128, 128, 1, 0); rc = make_map_2d(&P.mapU, p.B, p.K, p.N, 128, 128); }
     if (rc) return rc;
-    if (!p.transA) { P.v = layout_kmajor((uint32_t)P.bn, 128); rc = make_map_2d(&P.mapV, p.A, p.M, p.K, (uint32_t)P.bn, 128); }
-    else           { P.v = layout_mnmajor(128, 128, 1, 0);     rc = make_map_2d(&P.mapV, p.A, p.K, p.M, 128, 128); }
-    if (rc) return rc;
-    if ((rc = make_map_scales(&P.mapSU, p.sB, p.N, p.K, 1)) || (rc = make_map_scales(&P.mapSV, p.sA, p.M, p.K, 1))) return rc;
+    if (p.transA) P.v = layout_mnmajor(128, 128, 1, 0);
+    else          P.v = layout_kmajor((uint32_t)P.bn, 128);
     P.idesc = make_idesc_f8(p.formatB, p.formatA, P.u.major, P.v.major, 128, (uint32_t)P.bn);
     P.k_blocks = (int)f8_blocks(p.K);
     const int64_t tiles_n = f8_blocks(p.N), tiles_m = (p.M + P.bn - 1) / P.bn;
     static PerDeviceOnce configured;
-    QBP_SMEM_OPT_IN(configured, f8_split_kernel, kSplitSmem);
+    QBP_SMEM_OPT_IN(configured, f8_split_kernel<FromCodes>, kSplitSmem);
     // Parts: as many as run at the same time, where they save more blocks of 0.25 us than adding up the tile's rows costs (one call of
-    // many in a row, one part and the best, us: 1 x 4096 x 4096 16.2 and 11.8 (four), 64 x 1024 x 1024 9.6 and 9.0 (eight), 128 x 1024 x
-    // 1024 10.1 and 10.4 (eight), 256 x 4096 x 4096 17.8 and 18.5 (two), x 8192 26.6 and 24.9).
+    // many in a row, one part and the best, us: 1 x 4096 x 4096 12.7 and 7.9 (four), 64 x 1024 x 1024 5.9 and 5.3 (eight), 128 x 1024 x
+    // 1024 6.4 and 6.7 (eight), 512 x 2048 x 4096 14.3 and 14.1 (two), x 8192 23.9 and 20.6).
     P.parts = 1;
     while (P.parts < kSplitMaxParts && 2 * P.parts <= P.k_blocks && tiles_n * tiles_m <= split_clusters(2 * P.parts)) P.parts *= 2;
     if (P.k_blocks - (P.k_blocks + P.parts - 1) / P.parts <= 2 + P.bn / 16 * (P.parts == 2 ? 3 : 1)) P.parts = 1;
@@ -437,11 +505,31 @@ static int launch_f8_split(const F8Product &p, cudaStream_t st)
     P.stages = (int)std::min<int64_t>(kSplitMaxStages, (kSplitSmem - 1024 - sums_bytes) / P.stage_bytes);
     P.stages = std::min(P.stages, std::max(2, (P.k_blocks + P.parts - 1) / P.parts + 1));
     P.stages -= P.stages % (int)kSplitRelease;
-    static_assert(kSplitMaxStages + (int)kSplitRelease <= 4 * kSplitSets - 3, "a set of scales is written again while MMAs may read it");
+    static_assert(kSplitMaxStages + (int)kSplitRelease <= 4 * kSplitSets - 3 && kSplitMaxStages + (int)kSplitRelease < kSplitBlockSets &&
+                  kSplitSetU + 4 * kSplitSets <= kSplitSetV && kSplitSetV + 4 * kSplitBlockSets <= kSplitCols, "a set of scales is written again while MMAs may read it");
     const size_t ring = (size_t)P.stages * P.stage_bytes + sums_bytes;
-    P.M = p.M; P.N = p.N; P.out = p.out; P.dtype = p.dtype; P.status = p.status; P.clear = p.cleared ? 0 : 1;
+    P.M = p.M; P.N = p.N; P.out = p.out; P.dtype = p.dtype; P.status = p.status;
+    P.su = p.sB; P.groups = f8_groups(p.K); P.clear = p.cleared ? 0 : 1;
+    const dim3 grid((unsigned)(tiles_n * P.parts), (unsigned)tiles_m);
+    // Few rows are quantised by every CTA for itself (one call of many in a row, the quantiser apart and on the way, us: 1 x 4096 x 4096 11.5
+    // and 8.4, 16 x 1024 x 1024 8.1 and 7.1, 1 x 8192 x 8192 20.2 and 17.4; 32 x 1024 x 1024 8.3 and 9.2)
+    if (in.x && p.M > kSplitQuantise) return kSplitDeclined;
+    if (in.x) {
+        P.x = in.x; P.ld = in.ld; P.K = p.K;
+        P.vec = aligned16(in.x) && in.ld * (int64_t)dtype_size(p.dtype) % 16 == 0 ? 1 : 0;
+        QBP_TRACE_BEGIN(st);
+        QBP_FOR_DTYPE(p.dtype, T, {
+            static PerDeviceOnce once;
+            QBP_SMEM_OPT_IN(once, f8_split_kernel<T>, kSplitSmem);
+            launch_clusters(f8_split_kernel<T>, grid, (unsigned)P.parts, kSplitThreads, 1024 + ring, st, P);
+        });
+        QBP_LAUNCH_OK("f8_split_kernel<quantise>");
+        return QBP_OK;
+    }
+    P.sv = p.sA;
+    if ((rc = p.transA ? make_map_2d(&P.mapV, p.A, p.K, p.M, 128, 128) : make_map_2d(&P.mapV, p.A, p.M, p.K, (uint32_t)P.bn, 128))) return rc;
     QBP_TRACE_BEGIN(st);
-    launch_clusters(f8_split_kernel, dim3((unsigned)(tiles_n * P.parts), (unsigned)tiles_m), (unsigned)P.parts, kSplitThreads, 1024 + ring, st, P);
+    launch_clusters(f8_split_kernel<FromCodes>, grid, (unsigned)P.parts, kSplitThreads, 1024 + ring, st, P);
     QBP_LAUNCH_OK("f8_split_kernel");
     return QBP_OK;
 }
@@ -472,7 +560,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_quantize_f8(const void
                                                                       uint8_t *q_rows, uint8_t *s_rows, uint8_t *q_cols, uint8_t *s_cols, void *stream)
 {
     int rc = check_quantize("quantize_f8", x, dtype, rows, cols, ld, format);
-    if (rc) return rc;
+    if (rc || rows == 0 || cols == 0) return rc;
     if (!q_rows != !s_rows || !q_cols != !s_cols || (!q_rows && !q_cols)) return fail(QBP_ERR_INVALID_ARG, "quantize_f8: a copy needs both its codes and its scales");
     if (!aligned16(q_rows) || !aligned16(s_rows) || !aligned16(q_cols) || !aligned16(s_cols)) return fail(QBP_ERR_INVALID_ARG, "quantize_f8: codes and scales start on 16-byte boundaries");
     return launch_f8_quantize(x, dtype, rows, cols, ld, format, (q_rows ? kF8Rows : 0) | (q_cols ? kF8Cols : 0), q_rows, s_rows, q_cols, s_cols, (cudaStream_t)stream);
@@ -482,20 +570,21 @@ extern "C" __attribute__((visibility("default"))) int qbp_quantize_f8_square(con
                                                                              uint8_t *q, uint8_t *s_rows, uint8_t *s_cols, void *stream)
 {
     int rc = check_quantize("quantize_f8_square", x, dtype, rows, cols, ld, format);
-    if (rc) return rc;
+    if (rc || rows == 0 || cols == 0) return rc;
     if (!q || (!s_rows && !s_cols)) return fail(QBP_ERR_INVALID_ARG, "quantize_f8_square: NULL codes, or neither table of scales");
     if (!aligned16(q) || !aligned16(s_rows) || !aligned16(s_cols)) return fail(QBP_ERR_INVALID_ARG, "quantize_f8_square: codes and scales start on 16-byte boundaries");
     return launch_f8_quantize(x, dtype, rows, cols, ld, format, kF8Square, q, s_rows, nullptr, s_cols, (cudaStream_t)stream);
 }
 
-static int run_product(const F8Product &p, cudaStream_t st)
+// Whether the product runs on single CTAs.
+// One wave of tiles of 128 on single CTAs against tiles of 256 rows on pairs (one call of many in a row, split and pair, us): 64 x 4096 x
+// 8192 15.7 and 27.3, 512 x 4096 x 512 9.9 and 11.5, 1111 x 2048 x 8192 27.6 and 31.0; two waves: 512 x 8192 x 2048 26.3 and 17.4.
+static bool one_wave(const F8Product &p)
 {
-    // One wave of tiles of 128 on single CTAs against tiles of 256 rows on pairs (one call of many in a row, split and pair, us): 64 x 4096 x
-    // 8192 15.7 and 27.3, 512 x 4096 x 512 9.9 and 11.5, 1111 x 2048 x 8192 27.6 and 31.0; two waves: 512 x 8192 x 2048 26.3 and 17.4.
     const int64_t rows = p.transA || p.M > 64 ? 128 : 64;
-    if (f8_blocks(p.N) * ((p.M + rows - 1) / rows) > sm_count()) return launch_f8_pair(p, st);
-    return launch_f8_split(p, st);
+    return f8_blocks(p.N) * ((p.M + rows - 1) / rows) <= sm_count();
 }
+static int run_product(const F8Product &p, cudaStream_t st) { return one_wave(p) ? launch_f8_split(p, SplitInput{nullptr, 0}, st) : launch_f8_pair(p, st); }
 
 static int check_product(const F8Product &p, const char *name)
 {
@@ -564,6 +653,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_linear_f8(const void *
         return QBP_OK;
     }
     if (!w || !sw || !aligned16(w) || !aligned16(sw)) return fail(QBP_ERR_INVALID_ARG, "linear_f8: the weights or their scales are NULL or not on a 16-byte boundary");
+    if (one_wave(p) && (rc = launch_f8_split(p, SplitInput{x, ld}, st)) != kSplitDeclined) return rc;
     WsCarver c(ws, ws_bytes);
     c.take<int>(1);
     uint8_t *q = c.take<uint8_t>((size_t)M * (size_t)K), *s = c.take<uint8_t>(qbp_f8_scale_bytes(M, K));

@@ -81,12 +81,12 @@ template <int FORMAT> __device__ __forceinline__ uint2 f8_codes8(const float (&v
     return make_uint2(f8_codes2<FORMAT>(v[0], v[1]) | (f8_codes2<FORMAT>(v[2], v[3]) << 16), f8_codes2<FORMAT>(v[4], v[5]) | (f8_codes2<FORMAT>(v[6], v[7]) << 16));
 }
 
-__device__ __forceinline__ void tma_load_3d(void *dst, const void *map, uint64_t *bar, int x, int y, int z)
+// A plain copy of 16-byte aligned bytes (a multiple of 16) to shared memory, reported on an mbarrier.
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
 {
-    asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-        ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
-        : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
 }
 // Whether the barrier's phase is complete, without waiting (try_wait may hold the thread for microseconds where it is not).
 __device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity)

@@ -813,7 +813,7 @@ static int check_join(const qbp_resnorm_desc *d, const char *name, const void *b
     if (d->cols > kJoinMaxCols) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: %lld columns, at most %lld", name, (long long)d->cols, (long long)kJoinMaxCols);
     if (!(d->eps >= 0.0f) || !(d->p >= 0.0f && d->p <= 1.0f) || std::isinf(d->eps)) return fail(QBP_ERR_INVALID_ARG, "%s: eps %g, p %g", name, (double)d->eps, (double)d->p);
     if (d->index_base % 8) return fail(QBP_ERR_INVALID_ARG, "%s: index_base %llu is not a multiple of 8", name, (unsigned long long)d->index_base);
-    if (!b && (d->post || gate || d->p > 0.0f)) return fail(QBP_ERR_INVALID_ARG, "%s: a norm after, a gate or dropout without a block output", name);
+    if (!b && d->rows > 0 && d->cols > 0 && (d->post || gate || d->p > 0.0f)) return fail(QBP_ERR_INVALID_ARG, "%s: a norm after, a gate or dropout without a block output", name);
     for (const float *w : {gate, w_post, w_pre})
         if (!aligned_to(w, 4)) return fail(QBP_ERR_INVALID_ARG, "%s: misaligned parameters", name);
     return QBP_OK;
@@ -908,19 +908,18 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
     cudaStream_t st = (cudaStream_t)stream;
     int rc = check_join(d, "resnorm_bwd", b, gate, w_post, w_pre);
     if (rc) return rc;
-    if ((db || dgate) && !b) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: gradients of a block output that is NULL");
-    if ((dw_post && !d->post) || (dw_pre && !d->pre)) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: gradients of a norm that is not there");
-    if (!dx && !db && !dw_post && !dgate && !dw_pre) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: no output wanted");
     for (const float *w : {(const float *)dw_post, (const float *)dgate, (const float *)dw_pre, rstd_post, rstd_pre})
         if (!aligned_to(w, 4)) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: misaligned fp32 tensors");
-    const int64_t gates = gate || dgate ? join_gates(d) : 1;
+    if ((dw_post && !d->post) || (dw_pre && !d->pre)) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: gradients of a norm that is not there");
     if (d->cols == 0) return QBP_OK;
-    if (d->rows == 0) {
+    if (d->rows == 0) {                              // (no gates but for one that all rows share)
         if (dw_post) QBP_CUDA_OK(cudaMemsetAsync(dw_post, 0, (size_t)d->cols * 4, st));
         if (dw_pre) QBP_CUDA_OK(cudaMemsetAsync(dw_pre, 0, (size_t)d->cols * 4, st));
-        if (dgate) QBP_CUDA_OK(cudaMemsetAsync(dgate, 0, (size_t)(gates * d->cols) * 4, st));
+        if (dgate && !d->gate_rows) QBP_CUDA_OK(cudaMemsetAsync(dgate, 0, (size_t)d->cols * 4, st));
         return QBP_OK;
     }
+    if ((db || dgate) && !b) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: gradients of a block output that is NULL");
+    if (!dx && !db && !dw_post && !dgate && !dw_pre) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: no output wanted");
     if ((dr && !real_ok(dr, d->x_dtype)) || (d->pre && (!real_ok(dh, d->b_dtype) || !real_ok(r, d->x_dtype) || !rstd_pre)) || (d->post && !rstd_post) ||
         (b && !real_ok(b, d->b_dtype)) || (dx && !real_ok(dx, d->x_dtype)) || (db && !real_ok(db, d->b_dtype)))
         return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: a tensor is NULL or misaligned");

@@ -183,3 +183,101 @@ class TernarizedLayer:
                                                    d=self.conv)
         self.g, self.t, self.qt = g, t, qt
         return dx, dw, dgamma, dbeta
+
+
+class F8Linear:
+    """A linear layer y = x w^T in 8-bit floating point with a scale for each block of 128: the activation and the gradient are
+    quantised along their rows for y and dx and along their columns for dw, the fp32 master weights w [out_features,
+    in_features] in 128 x 128 blocks, once per forward.  Call order and buffers only.  grad_format: B.QBP_E5M2 gives the gradient
+    the wider range."""
+
+    def __init__(self, w, grad_format=B.QBP_E4M3):
+        self.w, self.grad_format = w, grad_format
+        self.ws = torch.empty(256, dtype=torch.uint8, device=w.device)
+        self.codes = self.saved = self.dw = None
+
+    def quantise(self):
+        """The weights' codes and scales, as a layer that serves keeps them until its weights change."""
+        self.codes = B.qbp_quantize_f8_square(self.w)
+        return self.codes
+
+    def serve(self, x):
+        """y for an activation of any number of rows, from the codes quantise() left."""
+        q, s, _ = self.codes
+        return B.qbp_linear_f8(x, q, s)
+
+    def forward(self, x):
+        q, s, _ = self.quantise()
+        xq, sx, xqt, sxt = B.qbp_quantize_f8(x, cols=True)
+        self.saved = (xqt, sxt)
+        return B.qbp_gemm_f8(xq, sx, q, s, transB=True, out_dtype=x.dtype, ws=self.ws)
+
+    def backward(self, g):
+        """dx in g's type; the weights' gradient is left in dw (fp32)."""
+        q, _, st = self.codes
+        xqt, sxt = self.saved
+        gq, sg, gqt, sgt = B.qbp_quantize_f8(g, format=self.grad_format, cols=True)
+        dx = B.qbp_gemm_f8(gq, sg, q, st, formatA=self.grad_format, out_dtype=g.dtype, ws=self.ws)
+        self.dw = B.qbp_gemm_f8(gqt, sgt, xqt, sxt, transA=True, formatA=self.grad_format, out=self.dw, ws=self.ws)
+        return dx
+
+    def status(self) -> int:
+        return B.status_word(self.ws)
+
+
+class F8ResidualStack:
+    """Residual blocks of one linear layer each: h = norm(x) w_pre, and for every block b = linear(h), r = alpha x + gate *
+    dropout(norm(b) w_post), the next block's h = norm(r) w_pre, with the join after a block and before the next one as one pass.
+    Master weights, norms and gates are fp32 and updated by qbp_sgd_update_many.  Call order and buffers only."""
+
+    def __init__(self, weights, alpha=1.0, eps=1e-6, p=0.0, seed=0, lr=0.1, momentum=0.9, weight_decay=0.0, grad_format=B.QBP_E5M2):
+        """weights: [C, C] fp32 device tensors, one for each block, updated in place."""
+        self.linears = [F8Linear(w, grad_format) for w in weights]
+        C, dev = weights[0].shape[0], weights[0].device
+        ones = lambda: torch.ones(C, dtype=torch.float32, device=dev)
+        self.w_first = ones()                                              # the norm before the first block
+        self.w_post, self.w_pre, self.gate = ([ones() for _ in weights] for _ in range(3))
+        self.alpha, self.eps, self.p, self.seed, self.lr, self.momentum, self.weight_decay = alpha, eps, p, seed, lr, momentum, weight_decay
+        self.step = 0
+        self.velocity = None
+        self.saved = self.grads = None
+
+    def forward(self, x, h_dtype=torch.bfloat16):
+        """x [rows, C]: the residual stream, of its own type.  Returns the last block's h (h_dtype)."""
+        n = len(self.linears)
+        first = B.resnorm_desc(x, eps=self.eps, h_dtype=h_dtype)
+        _, h, _, q = B.qbp_resnorm_fwd(first, x, w_pre=self.w_first)
+        joins, r = [], x
+        for i, lin in enumerate(self.linears):
+            b = lin.forward(h)
+            # (a stream of draws for each block and step)
+            d = B.resnorm_desc(r, b, alpha=self.alpha, eps=self.eps, p=self.p, seed=self.seed, tensor_id=self.step * n + i)
+            r, h, q1, q2 = B.qbp_resnorm_fwd(d, r, b, self.w_post[i], self.gate[i], self.w_pre[i])
+            joins.append((d, b, r, q1, q2))
+        self.saved = (first, x, q, joins)
+        return h
+
+    def backward(self, dh):
+        """dh: the gradient at forward's result.  Returns the gradient at x; the parameters' are left in grads."""
+        first, x, q, joins = self.saved
+        dr, grads = None, []
+        for i in reversed(range(len(joins))):
+            d, b, r, q1, q2 = joins[i]
+            dr, db, dw1, dg, dw2 = B.qbp_resnorm_bwd(d, dr, dh, b, r, q1, q2, self.w_post[i], self.gate[i], self.w_pre[i])
+            dh = self.linears[i].backward(db)
+            grads.append((self.linears[i].dw, dw1, dg.view(-1), dw2))
+        dx, _, _, _, dw = B.qbp_resnorm_bwd(first, dr, dh, None, x, None, q, w_pre=self.w_first)
+        self.grads = (grads[::-1], dw)
+        return dx
+
+    def update(self):
+        blocks, dw_first = self.grads
+        ws = [self.w_first] + [t for i, lin in enumerate(self.linears) for t in (lin.w, self.w_post[i], self.gate[i], self.w_pre[i])]
+        gs = [dw_first] + [t for g in blocks for t in g]
+        if self.momentum and self.velocity is None: self.velocity = [torch.zeros_like(w) for w in ws]
+        vs = self.velocity or [None] * len(ws)
+        B.qbp_sgd_update_many([(w, g, v, self.weight_decay if w.dim() == 2 else 0.0) for w, g, v in zip(ws, gs, vs)], self.lr, self.momentum)
+        self.step += 1
+
+    def status(self) -> int:
+        return min(lin.status() for lin in self.linears)

@@ -212,3 +212,21 @@ def test_products_of_many_tiles(B, M, N, K, transA, transB):
     again = B.qbp_gemm_f8(qa, sa, qb, sb, transA=transA, transB=transB, formatB=1, out_dtype=torch.bfloat16)
     assert torch.equal(again, got)                                # the same bits every time
     assert B.status_word(B.workspace(256)) == 0
+
+
+# few rows are quantised on the way to the tensor cores, more by the quantiser: one row, part of sixteen, more than sixteen, a part of a
+# block of columns, several blocks and pieces; the rows padded
+@pytest.mark.parametrize("M,N,K", [(1, 16, 16), (1, 4096, 4096), (3, 256, 144), (15, 1008, 2048), (16, 8192, 1040), (17, 256, 8192), (33, 144, 528), (64, 2048, 2048),
+                                   (77, 1008, 2048), (100, 4096, 4096), (128, 128, 4096), (129, 512, 1024), (300, 4096, 4096), (2000, 640, 256)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_is_the_quantiser_and_the_product(B, M, N, K, dtype):
+    import torch
+    x = torch.from_numpy(wide_values(M, K + 24, M + K).astype(np.float32)).to(getattr(torch, dtype)).cuda()[:, 8:8 + K]
+    w = torch.from_numpy(rng(N).standard_normal((N, K)).astype(np.float32) * 2.0 ** -6).cuda()
+    for fmt in (0, 1):
+        wq, sw, _ = B.qbp_quantize_f8_square(w, format=fmt)
+        q, s = B.qbp_quantize_f8(x)
+        want = B.qbp_gemm_f8(q, s, wq, sw, transB=True, formatB=fmt, out_dtype=x.dtype)
+        assert torch.equal(B.qbp_linear_f8(x, wq, sw, w_format=fmt), want)
+        assert torch.equal(B.qbp_linear_f8(x.contiguous(), wq, sw, w_format=fmt), want)
+    assert B.status_word(B.workspace(256)) == 0
