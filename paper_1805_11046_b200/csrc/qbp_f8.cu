@@ -57,15 +57,41 @@ f8_quantize_kernel(const T *__restrict__ x, int64_t rows, int64_t cols, int64_t 
 #pragma unroll
         for (int i = 0; i < kQuantPasses; ++i) raw[i] = load8(in && 16 * i + high < here ? src + 16 * i * ld : x, in && 16 * i + high < here ? 8 : 0, false);
     }
-    float col_max[8] = {}, row_max[kQuantPasses];
+    float col_max[8], row_max[kQuantPasses];
+    if constexpr (sizeof(T) == 2) {
+        // two elements to a word
+        using Max = HalfMax<T>;
+        uint32_t c[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < kQuantPasses; ++i) {
-        float v[8];
-        unpack8(raw[i], v);
-        if (WHAT & (kF8Rows | kF8Square)) row_max[i] = amax3(amax3(amax3(amax3(v[0], v[1], v[2]), v[3], v[4]), v[5], v[6]), v[7], 0.0f);
-        if (WHAT & kF8Cols) {
+        for (int i = 0; i < kQuantPasses; ++i) {
+            const uint4 w = raw[i].w[0];
+            const uint32_t a[4] = {w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu, w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu};
+            if (WHAT & kF8Cols) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) col_max[e] = amax3(col_max[e], v[e], 0.0f);
+                for (int k = 0; k < 4; ++k) c[k] = Max::max2(c[k], a[k]);
+            }
+            if (WHAT & (kF8Rows | kF8Square)) {
+                const uint32_t m = Max::max2(Max::max2(a[0], a[1]), Max::max2(a[2], a[3]));
+                row_max[i] = Max::value(Max::max2(m, m >> 16), 0);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { col_max[2 * k] = Max::value(c[k], 0); col_max[2 * k + 1] = Max::value(c[k], 1); }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) col_max[e] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kQuantPasses; i += 2) {
+            float v[8], u[8];
+            unpack8(raw[i], v); unpack8(raw[i + 1], u);
+            if (WHAT & (kF8Rows | kF8Square)) {
+                row_max[i] = amax3(amax3(amax3(amax3(v[0], v[1], v[2]), v[3], v[4]), v[5], v[6]), v[7], 0.0f);
+                row_max[i + 1] = amax3(amax3(amax3(amax3(u[0], u[1], u[2]), u[3], u[4]), u[5], u[6]), u[7], 0.0f);
+            }
+            if (WHAT & kF8Cols) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) col_max[e] = amax3(col_max[e], v[e], u[e]);
+            }
         }
     }
     float col_inv[8], tile_inv = 1.0f;
@@ -106,33 +132,42 @@ f8_quantize_kernel(const T *__restrict__ x, int64_t rows, int64_t cols, int64_t 
             if (s_cols) put_scale(p_cols, threadIdx.x, b_cols, last_r, tile_c * kF8Block + threadIdx.x < cols ? byte : 127u);
         }
     }
-    uint8_t *const d_rows = q_rows + (r0 + high) * cols + c0, *const d_cols = q_cols + (r0 + high) * cols + c0;
+    float row_inv = 1.0f;                                     // of row 16 (lane16 / 2) + high
+    if (WHAT & kF8Rows) {
+        // The eight rows' maxima over the sixteen lanes, halving the rows a lane is concerned with at each exchange: lane 2 i ends with
+        // row 16 i + high, and works out its scale alone.
+        float a[4], b[2], m;
+        const bool up8 = (lane16 & 8) != 0, up4 = (lane16 & 4) != 0, up2 = (lane16 & 2) != 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = amax3(up8 ? row_max[j + 4] : row_max[j], __shfl_xor_sync(0xFFFFFFFFu, up8 ? row_max[j] : row_max[j + 4], 8), 0.0f);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) b[j] = amax3(up4 ? a[j + 2] : a[j], __shfl_xor_sync(0xFFFFFFFFu, up4 ? a[j] : a[j + 2], 4), 0.0f);
+        m = amax3(up2 ? b[1] : b[0], __shfl_xor_sync(0xFFFFFFFFu, up2 ? b[0] : b[1], 2), 0.0f);
+        m = amax3(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1), 0.0f);
+        const uint32_t byte = f8_scale_byte<FORMAT>(m);
+        row_inv = f8_inverse(byte);
+        if ((lane16 & 1) == 0) put_scale(p_rows, 8 * lane16 + high, b_rows, last_c, byte);         // (127 for rows behind the last)
+    }
+    uint8_t *d_rows = q_rows + (r0 + high) * cols + c0, *d_cols = q_cols + (r0 + high) * cols + c0;
 #pragma unroll
     for (int i = 0; i < kQuantPasses; ++i) {
-        const int r = 16 * i + high;
         float v[8], inv = tile_inv;
         unpack8(raw[i], v);
-        if (WHAT & kF8Rows) {
-            float m = row_max[i];
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) m = amax3(m, __shfl_xor_sync(0xFFFFFFFFu, m, o), 0.0f);
-            const uint32_t byte = f8_scale_byte<FORMAT>(m);
-            inv = f8_inverse(byte);
-            if (lane16 == 0) put_scale(p_rows, r, b_rows, last_c, byte);              // (127 for rows behind the last)
-        }
-        if (r < here && in) {
+        if (WHAT & kF8Rows) inv = __shfl_sync(0xFFFFFFFFu, row_inv, (threadIdx.x & 16) | (2 * i));
+        if (16 * i + high < here && in) {
             if (WHAT & (kF8Rows | kF8Square)) {
                 float t[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) t[e] = __fmul_rn(v[e], inv);
-                *reinterpret_cast<uint2 *>(d_rows + 16 * i * cols) = f8_codes8<FORMAT>(t);
+                for (int e = 0; e < 8; e += 2) { t[e] = v[e]; t[e + 1] = v[e + 1]; mul2(t[e], t[e + 1], inv, inv); }
+                *reinterpret_cast<uint2 *>(d_rows) = f8_codes8<FORMAT>(t);
             }
             if (WHAT & kF8Cols) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], col_inv[e]);
-                *reinterpret_cast<uint2 *>(d_cols + 16 * i * cols) = f8_codes8<FORMAT>(v);
+                for (int e = 0; e < 8; e += 2) mul2(v[e], v[e + 1], col_inv[e], col_inv[e + 1]);
+                *reinterpret_cast<uint2 *>(d_cols) = f8_codes8<FORMAT>(v);
             }
         }
+        d_rows += 16 * cols; d_cols += 16 * cols;
     }
 }
 

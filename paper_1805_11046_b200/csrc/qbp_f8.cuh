@@ -43,18 +43,28 @@ int launch_f8_pair(const F8Product &p, cudaStream_t st);
 
 #ifdef __CUDACC__
 
+template <typename T> struct IsBf16 { static constexpr bool value = false; };
+template <> struct IsBf16<__nv_bfloat16> { static constexpr bool value = true; };
+
 // Format constants: the largest value is 1.75 * 2^top.
 template <int FORMAT> struct F8Format;
 template <> struct F8Format<QBP_E4M3> { static constexpr int top = 8; };
 template <> struct F8Format<QBP_E5M2> { static constexpr int top = 15; };
 
-// Two values to codes, nearest with ties to even, saturating; the first in the low byte.
-template <int FORMAT> __device__ __forceinline__ uint32_t f8_codes2(float a, float b)
+// Four values to codes, nearest with ties to even, saturating, the first in the lowest byte; a NaN to the format's NaN (0x7F).
+template <int FORMAT> __device__ __forceinline__ uint32_t f8_codes4(float a, float b, float c, float d)
 {
-    uint16_t r;
-    if (FORMAT == QBP_E4M3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
-    else                    asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
+    uint32_t r;
+    if (FORMAT == QBP_E4M3)
+        asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}" : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
+    else
+        asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e5m2x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e5m2x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}" : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
     return r;
+}
+// Two products in one instruction.
+__device__ __forceinline__ void mul2(float &a, float &b, float x, float y)
+{
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tmul.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
 }
 // Largest magnitude of three; NaN if one of them is.
 __device__ __forceinline__ float amax3(float a, float b, float c)
@@ -75,12 +85,30 @@ template <int FORMAT> __device__ __forceinline__ uint32_t f8_scale_byte(float am
 }
 // 2^-e of a scale byte (e <= 120: a normal number, up to 2^127; NaN of 255)
 __device__ __forceinline__ float f8_inverse(uint32_t byte) { return byte == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((254u - byte) << 23); }
-// Eight scaled values to eight codes (a NaN to the format's NaN).
+// Eight scaled values to eight codes.
 template <int FORMAT> __device__ __forceinline__ uint2 f8_codes8(const float (&v)[8])
 {
-    return make_uint2(f8_codes2<FORMAT>(v[0], v[1]) | (f8_codes2<FORMAT>(v[2], v[3]) << 16), f8_codes2<FORMAT>(v[4], v[5]) | (f8_codes2<FORMAT>(v[6], v[7]) << 16));
+    return make_uint2(f8_codes4<FORMAT>(v[0], v[1], v[2], v[3]), f8_codes4<FORMAT>(v[4], v[5], v[6], v[7]));
 }
 
+// Largest magnitudes of eight elements and more, as they are held: of the halves two to a word.  A NaN is passed on.
+template <typename T> struct HalfMax {
+    uint32_t m[4] = {0, 0, 0, 0};
+    static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
+    {
+        uint32_t r;
+        if (sizeof(T) == 2 && IsBf16<T>::value) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static __device__ __forceinline__ float value(uint32_t w, int high)
+    {
+        const uint16_t h = (uint16_t)(high ? w >> 16 : w);
+        T t;
+        memcpy(&t, &h, 2);
+        return real_of(t);
+    }
+};
 // A plain copy of 16-byte aligned bytes (a multiple of 16) to shared memory, reported on an mbarrier.
 __device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
 {
