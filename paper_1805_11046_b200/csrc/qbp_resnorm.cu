@@ -435,11 +435,22 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
         if (rows.first + sub < rows.end) fetch(rows.first + sub, 0);
 #pragma unroll
         for (int k = 0; k < CH; ++k) join_gains(P.gate, P.post ? P.w_post : nullptr, rows.gate * cols, c0 + k * apart, in[k], gw[k]);
+        float next1 = 1.0f, next2 = 0.0f;             // 1 / RMS of the next row, read a row ahead
+        if (rows.first + sub < rows.end) {
+            if (P.post) next1 = __ldg(P.rstd_post + rows.first + sub);
+            if (P.pre) next2 = __ldg(P.rstd_pre + rows.first + sub);
+        }
         for (int64_t row = rows.first + sub; row < rows.end; row += subs, turn ^= 1) {
             const uint4 *slot = mine + turn * turn_units;
-            const float rstd1 = P.post ? __ldg(P.rstd_post + row) : 1.0f, rstd2 = P.pre ? __ldg(P.rstd_pre + row) : 0.0f;
-            if (row + subs < rows.end) { fetch(row + subs, turn ^ 1); cp_async_wait<1>(); }
-            else cp_async_wait<0>();
+            const float rstd1 = next1, rstd2 = next2;
+            if (row + subs < rows.end) {
+                if (P.post) next1 = __ldg(P.rstd_post + row + subs);
+                if (P.pre) next2 = __ldg(P.rstd_pre + row + subs);
+                fetch(row + subs, turn ^ 1);
+                cp_async_wait<1>();
+            } else {
+                cp_async_wait<0>();
+            }
             __syncwarp();
             const int64_t at = row * cols + c0;
             // Both means from one exchange: the second, of v w_post b, is linear in the first, m, with R = (dr + dh w_pre rstd_pre) - r m.
@@ -734,11 +745,11 @@ join_bwd_any_kernel(const __grid_constant__ JoinBwdParams P, const __grid_consta
 }
 #endif
 
-// out[o][c] = sum over `count` partial rows in [outs][count][cols], in a fixed order: sixteen threads of a column take every sixteenth, then
-// the sixteen are added up.
+// out[o][c] = sum over `count` partial rows in [outs][count][cols], in a fixed order: thirty-two warps of a block's 32 columns take every
+// thirty-second, eight loads at a time (a sum waits for its loads and for nothing else), then the thirty-two are added up.
 struct JoinSum { const float *part; float *out; int64_t outs, count; };
 struct JoinSums { JoinSum j[3]; int64_t cols; };
-constexpr int kSumHigh = 16;
+constexpr int kSumHigh = 32, kSumAhead = 8;
 __global__ void __launch_bounds__(32 * kSumHigh) join_sum_kernel(const __grid_constant__ JoinSums S)
 {
     __shared__ float s_part[kSumHigh][33];
@@ -750,24 +761,28 @@ __global__ void __launch_bounds__(32 * kSumHigh) join_sum_kernel(const __grid_co
         float s = 0.0f;
         if (c < S.cols) {
             const float *p = j.part + o * j.count * S.cols + c;
-#pragma unroll 4
-            for (int64_t k = high; k < j.count; k += kSumHigh) s += p[k * S.cols];
+            for (int64_t k = high; k < j.count; k += kSumHigh * kSumAhead) {
+                float v[kSumAhead];
+#pragma unroll
+                for (int a = 0; a < kSumAhead; ++a) v[a] = k + a * kSumHigh < j.count ? p[(k + a * kSumHigh) * S.cols] : 0.0f;
+#pragma unroll
+                for (int a = 0; a < kSumAhead; ++a) s += v[a];
+            }
         }
         s_part[high][lane] = s;
         __syncthreads();
-        if (high == 0 && c < S.cols) {
-            float v = 0.0f;
+        // each warp adds up a column
+        float v = s_part[lane][high];
 #pragma unroll
-            for (int k = 0; k < kSumHigh; ++k) v += s_part[k][lane];
-            j.out[o * S.cols + c] = v;
-        }
+        for (int q = 16; q > 0; q >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, q);
+        if (lane == 0 && (int64_t)blockIdx.x * 32 + high < S.cols) j.out[o * S.cols + (int64_t)blockIdx.x * 32 + high] = v;
         __syncthreads();
     }
 }
 
 // ================================================================= host side
 struct JoinShape { int ch, threads; bool warp; };
-constexpr size_t kJoinMaxRing = 200 * 1024, kJoinSmRings = 222 * 1024;        // of a block, of an SM
+constexpr size_t kJoinMaxRing = 224 * 1024, kJoinSmRings = 222 * 1024;        // of a block, of an SM
 // Shared memory of a block's ring: three rows forward, with one tensor of each type, and two backwards, with two.
 static size_t join_ring(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
 {
@@ -800,7 +815,7 @@ template <typename Params>
 static int launch_join(void (*kernel)(Params, PhiloxKeys), PerDeviceOnce &once, int64_t blocks, const JoinShape &s, size_t smem, cudaStream_t st, const Params &P,
                        const PhiloxKeys &keys)
 {
-    if (smem > 24 * 1024) QBP_SMEM_OPT_IN(once, kernel, kJoinMaxRing);       // (with the static arrays beside it, over 48 KB)
+    if (smem > 24 * 1024) QBP_SMEM_OPT_IN(once, kernel, s.warp ? (size_t)200 * 1024 : kJoinMaxRing);       // (with the static arrays beside it, over 48 KB)
     launch(kernel, dim3((unsigned)blocks), s.threads, smem, st, P, keys);
     return QBP_OK;
 }
