@@ -696,7 +696,8 @@ int qbp_linear_f8(const void *x, int dtype, int64_t ld, int64_t M, int64_t N, in
  * x and r have x_dtype, b and h b_dtype; rows of any number, cols up to
  * QBP_RESNORM_MAX_COLS, every tensor aligned to its element (16 bytes and cols a multiple of 8:
  * faster).  rstd_post / rstd_pre [rows] (nullable) receive 1 / RMS for the backward pass.
- * r may be x, and h may be b.
+ * r may be x, and h may be b.  ws: 256 bytes, whose first four are the device status word (see
+ * Conventions), of the backward pass as well.
  * ---------------------------------------------------------------------- */
 #define QBP_RESNORM_MAX_COLS 16384
 typedef struct {
@@ -711,7 +712,8 @@ typedef struct {
 } qbp_resnorm_desc;
 
 int qbp_resnorm_fwd(const qbp_resnorm_desc *d, const void *x, const void *b, const float *w_post, const float *gate,
-                    const float *w_pre, void *r, void *h, float *rstd_post, float *rstd_pre, void *stream);
+                    const float *w_pre, void *r, void *h, float *rstd_post, float *rstd_pre,
+                    void *ws, size_t ws_bytes, void *stream);
 
 /* Its gradients, from those of r and h (dr in x's type, nullable: nothing else uses r;
  * dh in b's type, wanted with pre):

@@ -114,7 +114,7 @@ def _load() -> C.CDLL:
     lib.qbp_gemm_f8_workspace_bytes.argtypes = lib.qbp_linear_f8_workspace_bytes.argtypes = [i64, i64, i64]
     lib.qbp_gemm_f8.argtypes = [C.c_int, C.c_int, i64, i64, i64, C.c_int, ptr, ptr, C.c_int, ptr, ptr, C.c_int, ptr, ptr, size, ptr]
     lib.qbp_linear_f8.argtypes = [ptr, C.c_int, i64, i64, i64, i64, C.c_int, ptr, ptr, ptr, ptr, size, ptr]
-    lib.qbp_resnorm_fwd.argtypes = [ptr] * 11
+    lib.qbp_resnorm_fwd.argtypes = [ptr] * 11 + [size, ptr]
     lib.qbp_resnorm_bwd_workspace_bytes.argtypes = [ptr]
     lib.qbp_resnorm_bwd.argtypes = [ptr] * 16 + [size, ptr]
     lib.qbp_dropout.argtypes = [ptr, C.c_int, i64, C.c_float, C.c_uint64, C.c_uint32, C.c_uint64, ptr, ptr]
@@ -620,10 +620,10 @@ def _gates(d) -> int:
     return -(-d.rows // d.gate_rows) if d.gate_rows else 1
 
 
-def qbp_resnorm_fwd(d: ResnormDesc, x, b=None, w_post=None, gate=None, w_pre=None, r=None, h=None, rstd_post=None, rstd_pre=None):
+def qbp_resnorm_fwd(d: ResnormDesc, x, b=None, w_post=None, gate=None, w_pre=None, r=None, h=None, rstd_post=None, rstd_pre=None, ws=None):
     """Returns (r, h, rstd_post, rstd_pre), None where there is none: r without a block output and alpha 1 is x itself, h and its
     rstd without a norm before the next block.  h has b's type (without b, the descriptor's)."""
-    device = _here(x, b, w_post, gate, w_pre, r, h, rstd_post, rstd_pre)
+    device = _here(x, b, w_post, gate, w_pre, r, h, rstd_post, rstd_pre, ws)
     rows, cols, xt, bt = d.rows, d.cols, d.x_dtype, d.b_dtype
     n = rows * cols
     if r is None and not (b is None and d.alpha == 1.0): r = torch.empty_like(x)
@@ -631,10 +631,11 @@ def qbp_resnorm_fwd(d: ResnormDesc, x, b=None, w_post=None, gate=None, w_pre=Non
         if h is None: h = torch.empty_like(b) if b is not None else _new(x.shape, _REALS[bt], device)
         if rstd_pre is None: rstd_pre = _new(rows, torch.float32, device)
     if d.post and rstd_post is None: rstd_post = _new(rows, torch.float32, device)
+    if ws is None: ws = _scratch(256, device)
     _check(lib.qbp_resnorm_fwd(C.addressof(d), _real(x, n, xt, "x"), _real(b, n, bt, "b"), _real(w_post, cols, QBP_F32, "w_post"),
                                _real(gate, _gates(d) * cols, QBP_F32, "gate"), _real(w_pre, cols, QBP_F32, "w_pre"),
                                _real(r, n, xt, "r"), _real(h, n, bt, "h"), _real(rstd_post, rows, QBP_F32, "rstd_post"),
-                               _real(rstd_pre, rows, QBP_F32, "rstd_pre"), _stream_handle(device)))
+                               _real(rstd_pre, rows, QBP_F32, "rstd_pre"), ws.data_ptr(), ws.numel(), _stream_handle(device)))
     return r, h, rstd_post, rstd_pre
 
 

@@ -484,6 +484,13 @@ __device__ __forceinline__ void tma_load_4d(void *dst, const void *map, uint64_t
         ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
+// A plain copy of 16-byte aligned bytes (a multiple of 16) to shared memory, reported on an mbarrier.
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
 // TMA tiled stores (shared -> global) as bulk groups of the issuing thread; elements of the box that fall
 // outside the tensor are not written.  The x coordinate times the element size must be a multiple of 16.
 __device__ __forceinline__ void tma_store_2d(const void *map, const void *src, int x, int y)

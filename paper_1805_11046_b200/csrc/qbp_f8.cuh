@@ -109,13 +109,6 @@ template <typename T> struct HalfMax {
         return real_of(t);
     }
 };
-// A plain copy of 16-byte aligned bytes (a multiple of 16) to shared memory, reported on an mbarrier.
-__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
-{
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar))
-                 : "memory");
-}
 // Whether the barrier's phase is complete, without waiting (try_wait may hold the thread for microseconds where it is not).
 __device__ __forceinline__ bool mbar_test(uint64_t *bar, uint32_t parity)
 {

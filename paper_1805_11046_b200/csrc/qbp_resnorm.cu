@@ -6,8 +6,8 @@
 // gradients' projections on r and b) are exchanged between the group's threads, forward a row's second with the next row's first, backwards
 // both at once, and nothing is read twice.  A block
 // takes neighbouring rows of one gate (an item) and keeps the parameters of its columns in registers.  Rows come through a ring of two
-// or three in shared memory that each thread fills and reads for itself (cp.async, no barrier): a row is on its way while the one before is worked on,
-// and stays out of the threads' registers.
+// or three in shared memory, copied whole by one thread (cp.async.bulk): a row is on its way while the one before is worked on, and stays
+// out of the threads' registers.  (Copied by the threads that read it, 16 bytes each, a row of 48 KB took 2100 cycles of their time, of 5900.)
 //
 // Backwards, with gate and w_post constant along an item's columns, dw_post and dgate are multiples of one sum over its rows,
 // S = sum of R dropout'(b rstd_post): dgate = w_post S, dw_post = gate S.  A thread keeps S and dw_pre's sum in registers, a block leaves
@@ -33,6 +33,7 @@ struct JoinParams {
     void *r, *h; float *rstd_post, *rstd_pre;
     float eps, alpha, inv_cols;
     int post, pre, drop, x_dtype, b_dtype, wide;      // wide: outputs of fp32 start on 32-byte boundaries
+    int *status;
     DropoutParams d;
 };
 
@@ -42,6 +43,7 @@ struct JoinBwdParams {
     void *dx, *db; float *part_post, *part_gate, *part_pre;
     float alpha, inv_cols;
     int post, pre, drop, x_dtype, b_dtype, wide, sum_post, sum_gate, sum_pre;
+    int *status;
     DropoutParams d;
 };
 
@@ -143,10 +145,10 @@ template <bool VEC> struct Kept {
 };
 
 // Sums over the threads of a row's group, N at a time; every thread gets them.  WARP: the group is a warp.  `turn` alternates between
-// the two halves of the scratch, so that one barrier an exchange is enough.
+// the two halves of the scratch, so that one barrier an exchange is enough; `warps` take part.
 constexpr int kJoinSums = 3;
 typedef float JoinScratch[2][kJoinSums][16];
-template <bool WARP, int N> __device__ __forceinline__ void group_sums(float (&v)[N], JoinScratch &scratch, int turn)
+template <bool WARP, int N> __device__ __forceinline__ void group_sums(float (&v)[N], JoinScratch &scratch, int turn, int warps)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
@@ -157,19 +159,19 @@ template <bool WARP, int N> __device__ __forceinline__ void group_sums(float (&v
 #pragma unroll
         for (int n = 0; n < N; ++n) scratch[turn][n][threadIdx.x >> 5] = v[n];
     }
-    __syncthreads();
+    named_barrier(1, 32 * warps);
     // (every warp adds up the warps' sums by itself: one load a lane and four exchanges)
 #pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = (threadIdx.x & 15) < blockDim.x / 32 ? scratch[turn][n][threadIdx.x & 15] : 0.0f;
+    for (int n = 0; n < N; ++n) v[n] = (int)(threadIdx.x & 15) < warps ? scratch[turn][n][threadIdx.x & 15] : 0.0f;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1)
 #pragma unroll
         for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xFFFFFFFFu, v[n], o);
 }
-template <bool WARP> __device__ __forceinline__ float group_sum(float v, JoinScratch &scratch, int turn)
+template <bool WARP> __device__ __forceinline__ float group_sum(float v, JoinScratch &scratch, int turn, int warps)
 {
     float a[1] = {v};
-    group_sums<WARP>(a, scratch, turn);
+    group_sums<WARP>(a, scratch, turn, warps);
     return a[0];
 }
 
@@ -192,26 +194,54 @@ template <bool WARP> __device__ __forceinline__ void end_row(int pre, int post)
 }
 
 // ---- rows read in vectors, through the ring ------------------------------------------------------------------------------
-// A thread's 16-byte pieces of a row lie side by side in its slot, an odd number of them (so that the slots of a quarter warp
-// fall into different banks), a slot for each of two turns.  Pieces behind the last column are cleared once and never written.
+// A row is copied by a lane of its group's first warp, whose bytes a slot's barrier reports (full).  Forward a slot is free for the next
+// copy once its row's sums have been exchanged; backwards, where a row is read behind the exchange too, each warp says so (empty).  Every wait
+// is bounded: a warp whose wait ran out raises the status word, waits for nothing any more and goes through the rest of its rows for
+// the block's barriers' sake.
 template <typename T> struct Pieces { static constexpr int n = sizeof(T) / 2; };
-// The lanes of a warp copy 256 columns side by side, 16 bytes each at a time, into the slots of whoever reads them: of fp32 a lane's eight
-// columns are two such pieces, and copied by their reader each request would ask for half of 32 sectors.  slots: the first lane's; c: the
-// warp's first column.
-template <typename T, int SLOT> __device__ __forceinline__ void ring_fetch(uint4 *slots, const void *row0, int64_t at, int c, int cols)
+constexpr int kJoinSlots = 3, kJoinBackSlots = 2;
+struct JoinBars { uint64_t full[kJoinWarpRows][kJoinSlots], empty[kJoinBackSlots]; };
+__device__ __forceinline__ void join_bars_init(JoinBars &bars, int warps)
 {
-    constexpr int n = Pieces<T>::n;
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-        const int piece = 32 * i + (threadIdx.x & 31);
-        if (c + piece * (8 / n) < cols) cp_async16(slots + piece / n * SLOT + piece % n, static_cast<const T *>(row0) + at + piece * (8 / n));
+    if (threadIdx.x == 0) {
+        for (int w = 0; w < kJoinWarpRows; ++w)
+            for (int k = 0; k < kJoinSlots; ++k) mbar_init(&bars.full[w][k], 1);
+        for (int k = 0; k < kJoinBackSlots; ++k) mbar_init(&bars.empty[k], (uint32_t)warps);
+        mbar_fence_init();
     }
+    __syncthreads();
 }
-template <typename T> __device__ __forceinline__ void ring_read(const uint4 *slot, float (&v)[8])
+struct JoinSource { const void *row0; uint32_t row_bytes, offset; };        // offset: of the tensor's row in a slot
+// One row of each tensor into a slot, by a converged warp.
+template <int N> __device__ __forceinline__ void join_copy(uint8_t *slot, uint64_t *full, const JoinSource (&src)[N], int64_t row)
+{
+    if (elect_one()) {
+        uint32_t bytes = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) bytes += src[k].row0 ? src[k].row_bytes : 0u;
+        mbar_expect_tx(full, bytes);
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (src[k].row0) bulk_load(slot + src[k].offset, static_cast<const char *>(src[k].row0) + row * src[k].row_bytes, src[k].row_bytes, full);
+    }
+    __syncwarp();
+}
+// A warp's place in a ring of slots.
+struct JoinPlace {
+    uint32_t slot, ph;
+    __device__ __forceinline__ JoinPlace next(uint32_t slots) const { return slot + 1 == slots ? JoinPlace{0u, ph ^ 1u} : JoinPlace{slot + 1, ph}; }
+};
+__device__ __forceinline__ void join_wait(uint64_t *bar, uint32_t parity, bool &dead, int *status)
+{
+    if (!dead && !mbar_wait_uniform(bar, parity)) { dead = true; raise_timeout(status); }
+}
+// Eight columns of a row in a slot (zero behind the last one).
+template <typename T> __device__ __forceinline__ void ring_read(const uint8_t *row, int c, bool in, float (&v)[8])
 {
     Raw8<T> r;
+    const uint4 *p = reinterpret_cast<const uint4 *>(row + c * (int)sizeof(T));
 #pragma unroll
-    for (int i = 0; i < Pieces<T>::n; ++i) r.w[i] = slot[i];
+    for (int i = 0; i < Pieces<T>::n; ++i) r.w[i] = in ? p[i] : make_uint4(0, 0, 0, 0);
     unpack8(r, v);
 }
 // (wide: fp32 rows start on 32-byte boundaries)
@@ -239,105 +269,104 @@ __device__ __forceinline__ void join_gains(const float *gate, const float *w_pos
     }
 }
 
-template <typename TX, typename TB, int CH, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kJoinWarpRows : 512, WARP ? 2 : 1)
+template <typename TX, typename TB, int CH, bool WARP, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 2 : 1)
 join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ PhiloxKeys keys)
 {
-    extern __shared__ uint4 ring[];
+    extern __shared__ __align__(16) uint8_t ring[];
     __shared__ JoinScratch scratch;
-    constexpr int px = Pieces<TX>::n, pb = Pieces<TB>::n, kSlot = (CH * (px + pb)) | 1;
-    const int lane = threadIdx.x & 31, warp = WARP ? 0 : threadIdx.x >> 5, warps = WARP ? 1 : blockDim.x >> 5;
+    __shared__ JoinBars bars;
+    const int lane = threadIdx.x & 31, all_warps = (int)(blockDim.x >> 5), warp = WARP ? 0 : threadIdx.x >> 5, warps = WARP ? 1 : all_warps;
     const int sub = WARP ? threadIdx.x >> 5 : 0, subs = WARP ? kJoinWarpRows : 1;
     const int cols = (int)P.it.cols, c0 = 256 * warp + 8 * lane, apart = 256 * warps;      // the thread's first column, and its next ones'
-    const int turn_units = blockDim.x * kSlot;
-    uint4 *const mine = ring + threadIdx.x * kSlot;
+    const uint32_t row_x = (uint32_t)cols * sizeof(TX), row_b = (uint32_t)cols * sizeof(TB), slot_bytes = row_x + row_b;
+    join_bars_init(bars, all_warps);
+    pdl_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;          // (a wait gives up a second later at the earliest)
+    uint8_t *const slots = ring + (uint32_t)(sub * kJoinSlots) * slot_bytes;
+    uint64_t *const full = bars.full[sub];
+    const JoinSource src[2] = {{P.x, row_x, 0u}, {P.b, row_b, row_x}};
+    const auto fetch = [&](int64_t row, int64_t end, uint32_t slot) {
+        if ((WARP || warp == 0) && row < end) join_copy<2>(slots + slot * slot_bytes, &full[slot], src, row);
+    };
     bool in[CH];
     float gw[CH][8], w2[CH][8];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         in[k] = c0 + k * apart < cols;
-        for (int i = 0; i < px + pb; ++i)
-            if (!in[k] || (!P.b && i >= px))
-                for (int t = 0; t < 3; ++t) mine[t * turn_units + k * (px + pb) + i] = make_uint4(0, 0, 0, 0);
+        join_gains(P.w_pre, nullptr, 0, c0 + k * apart, in[k], w2[k]);
     }
-    const auto fetch = [&](int64_t row, int64_t end, uint4 *slot) {
-        const int c = 256 * warp;
-        const int64_t at = row * cols + c;
-        slot -= lane * kSlot;
-        __syncwarp();                                  // (every lane has read what the slots held)
-#pragma unroll
-        for (int k = 0; k < CH; ++k)
-            if (row < end) {
-                ring_fetch<TX, kSlot>(slot + k * (px + pb), P.x, at + k * apart, c + k * apart, cols);
-                if (P.b) ring_fetch<TB, kSlot>(slot + k * (px + pb) + px, P.b, at + k * apart, c + k * apart, cols);
-            }
-        cp_async_commit();
-    };
-    const auto square_sum = [&](const uint4 *slot) {
+    const auto square_sum = [&](uint32_t slot) {
         float s = 0.0f;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             float v[8];
-            ring_read<TB>(slot + k * (px + pb) + px, v);
+            ring_read<TB>(slots + slot * slot_bytes + row_x, c0 + k * apart, in[k], v);
 #pragma unroll
             for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
         }
         return s;
     };
-    pdl_wait();
-#pragma unroll
-    for (int k = 0; k < CH; ++k) join_gains(P.w_pre, nullptr, 0, c0 + k * apart, in[k], w2[k]);
     const float factor = P.drop ? P.d.factor : 1.0f;
     int64_t had = -1;
     int half = 0;
+    JoinPlace place{0u, 0u};
+    bool dead = false;
     for (int64_t item = blockIdx.x; item < P.it.gates * P.it.splits; item += gridDim.x) {
         const ItemRows rows = item_rows(P.it, item);
-        uint4 *slot = mine, *slot1 = mine + turn_units, *slot2 = mine + 2 * turn_units;
-        fetch(rows.first + sub, rows.end, slot);
-        fetch(rows.first + sub + subs, rows.end, slot1);
         if (P.b && rows.gate != had) {
 #pragma unroll
             for (int k = 0; k < CH; ++k) join_gains(P.gate, P.post ? P.w_post : nullptr, rows.gate * cols, c0 + k * apart, in[k], gw[k]);
             had = rows.gate;
         }
-        cp_async_wait<1>();
-        __syncwarp();
+        // (all slots are free: the last rows' sums have been exchanged)
+        JoinPlace p = place;
+        for (int k = 0; k < kJoinSlots; ++k) { fetch(rows.first + sub + k * subs, rows.end, p.slot); p = p.next(kJoinSlots); }
         float rstd = 1.0f;
-        if (P.post) { rstd = rsqrtf(group_sum<WARP>(square_sum(slot), scratch, half) * P.inv_cols + P.eps); half ^= 1; }
+        if (rows.first + sub < rows.end) {
+            join_wait(&full[place.slot], place.ph, dead, P.status);
+            if (P.post) { rstd = rsqrtf(group_sum<WARP>(square_sum(place.slot), scratch, half, warps) * P.inv_cols + P.eps); half ^= 1; }
+        }
         for (int64_t row = rows.first + sub; row < rows.end; row += subs) {
-            fetch(row + 2 * subs, rows.end, slot2);
             const int64_t at = row * cols + c0;
-            if (P.post && P.rstd_post && warp == 0 && lane == 0) P.rstd_post[row] = rstd;
             const float scale = factor * rstd;
             float r[CH][8], sums[2] = {0.0f, 0.0f};           // of this row's r^2, of the next row's b^2
+            if (P.post && P.rstd_post && warp == 0 && lane == 0) P.rstd_post[row] = rstd;
+            {
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                ring_read<TX>(slot + k * (px + pb), r[k]);
+                for (int k = 0; k < CH; ++k) {
+                    ring_read<TX>(slots + place.slot * slot_bytes, c0 + k * apart, in[k], r[k]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) r[k][e] *= P.alpha;
-                if (P.b) {
-                    float b[8];
-                    ring_read<TB>(slot + k * (px + pb) + px, b);
-                    if (P.drop) {                     // (what is dropped counts for nothing, whatever it is: chosen, not multiplied by zero)
-                        Kept<true> kept;
-                        kept.make(P.d, keys, P.drop, at - 8 * lane + k * apart, 0);
+                    for (int e = 0; e < 8; ++e) r[k][e] *= P.alpha;
+                    if (P.b) {
+                        float b[8];
+                        ring_read<TB>(slots + place.slot * slot_bytes + row_x, c0 + k * apart, in[k], b);
+                        if (P.drop) {                 // (what is dropped counts for nothing, whatever it is: chosen, not multiplied by zero)
+                            Kept<true> kept;
+                            kept.make(P.d, keys, P.drop, at - 8 * lane + k * apart, 0);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) b[e] = kept[e] ? b[e] : 0.0f;
+                            for (int e = 0; e < 8; ++e) b[e] = kept[e] ? b[e] : 0.0f;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) r[k][e] = fmaf(b[e] * scale, gw[k][e], r[k][e]);
                     }
+                    const Raw8<TX> raw = pack8<TX>(r[k]);
+                    if (P.r && in[k]) put_vec(P.r, at + k * apart, raw, P.wide);
+                    unpack8(raw, r[k]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) r[k][e] = fmaf(b[e] * scale, gw[k][e], r[k][e]);
+                    for (int e = 0; e < 8; ++e) sums[0] = fmaf(r[k][e], r[k][e], sums[0]);    // (zero behind the last column, as x and b are)
                 }
-                const Raw8<TX> raw = pack8<TX>(r[k]);
-                if (P.r && in[k]) put_vec(P.r, at + k * apart, raw, P.wide);
-                unpack8(raw, r[k]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sums[0] = fmaf(r[k][e], r[k][e], sums[0]);    // (zero behind the last column, as x and b are)
             }
-            cp_async_wait<1>();
+            const JoinPlace following = place.next(kJoinSlots);
+            if (row + subs < rows.end) {
+                join_wait(&full[following.slot], following.ph, dead, P.status);
+                if (P.post) sums[1] = square_sum(following.slot);
+            }
             __syncwarp();
-            if (P.post) sums[1] = square_sum(slot1);
-            group_sums<WARP>(sums, scratch, half);
+            group_sums<WARP>(sums, scratch, half, warps);
             half ^= 1;
+            fetch(row + kJoinSlots * subs, rows.end, place.slot);
+            place = following;
             rstd = P.post ? rsqrtf(sums[1] * P.inv_cols + P.eps) : 1.0f;
             if (P.pre) {
                 const float rstd2 = rsqrtf(sums[0] * P.inv_cols + P.eps);
@@ -349,18 +378,16 @@ join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ Ph
                     if (in[k]) put_vec(P.h, at + k * apart, pack8<TB>(r[k]), P.wide);
                 }
             }
-            uint4 *const t = slot; slot = slot1; slot1 = slot2; slot2 = t;
         }
-        cp_async_wait<0>();
     }
 }
 
 // A thread's sums of one kind over an item's rows to the block's partial row, times parameters of its columns (nullable).  added: to
 // what an item before of this block left there.  VEC: eight neighbouring columns, else 32 apart.
 template <int CH, bool WARP, bool VEC>
-__device__ __forceinline__ void join_leave(const float (&a)[CH][8], float *out, const float *w, int cols, int c0, int apart, bool added, float *fold)
+__device__ __forceinline__ void join_leave(const float (&a)[CH][8], float *out, const float *w, int cols, int c0, int apart, bool added, float *fold, int threads)
 {
-    if (WARP) __syncthreads();
+    if (WARP) named_barrier(1, threads);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         float m[8];
@@ -374,8 +401,8 @@ __device__ __forceinline__ void join_leave(const float (&a)[CH][8], float *out, 
         }
     }
     if (WARP) {
-        __syncthreads();
-        for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+        named_barrier(1, threads);
+        for (int c = threadIdx.x; c < cols; c += threads) {
             float s = added ? out[c] : 0.0f;
 #pragma unroll
             for (int q = 0; q < kJoinWarpRows; ++q) s += fold[q * 256 * CH + c];
@@ -384,155 +411,152 @@ __device__ __forceinline__ void join_leave(const float (&a)[CH][8], float *out, 
     }
 }
 
-template <typename TX, typename TB, int CH, bool WARP>
-__global__ void __launch_bounds__(WARP ? 32 * kJoinWarpRows : 512, 1)
+template <typename TX, typename TB, int CH, bool WARP, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == 256 && !WARP ? 2 : 1)
 join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__ PhiloxKeys keys)
 {
-    extern __shared__ uint4 ring[];
+    extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float fold[WARP ? kJoinWarpRows * 256 * CH : 1];            // WARP: the warps' sums
     __shared__ JoinScratch scratch;
-    // pieces of dr, r, dh, b
-    constexpr int px = Pieces<TX>::n, pb = Pieces<TB>::n, at_r = px, at_h = 2 * px, at_b = 2 * px + pb, row_units = 2 * (px + pb), kSlot = (CH * row_units) | 1;
-    const int lane = threadIdx.x & 31, warp = WARP ? 0 : threadIdx.x >> 5, warps = WARP ? 1 : blockDim.x >> 5;
+    __shared__ JoinBars bars;
+    const int lane = threadIdx.x & 31, all_warps = (int)(blockDim.x >> 5), warp = WARP ? 0 : threadIdx.x >> 5, warps = WARP ? 1 : all_warps;
     const int sub = WARP ? threadIdx.x >> 5 : 0, subs = WARP ? kJoinWarpRows : 1;
     const int cols = (int)P.it.cols, c0 = 256 * warp + 8 * lane, apart = 256 * warps;
-    const int turn_units = blockDim.x * kSlot;
-    uint4 *const mine = ring + threadIdx.x * kSlot;
+    const uint32_t row_x = (uint32_t)cols * sizeof(TX), row_b = (uint32_t)cols * sizeof(TB);
+    const uint32_t off_h = 2u * row_x, off_b = off_h + row_b, slot_bytes = off_b + row_b;          // dr, r, dh, b
+    join_bars_init(bars, all_warps);
+    pdl_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;          // (a wait gives up a second later at the earliest)
+    uint8_t *const slots = ring + (uint32_t)(sub * kJoinBackSlots) * slot_bytes;
+    uint64_t *const full = bars.full[sub];
+    const JoinSource src[4] = {{P.dr, row_x, 0u}, {P.pre ? P.r : nullptr, row_x, row_x}, {P.pre ? P.dh : nullptr, row_b, off_h}, {P.b, row_b, off_b}};
+    bool dead = false;
+    JoinPlace place{0u, 0u}, ahead{0u, 1u};          // of the row at hand, of the next row to be copied
+    const auto fetch = [&](int64_t row) {
+        if (WARP || warp == 0) {
+            if (!WARP) join_wait(&bars.empty[ahead.slot], ahead.ph, dead, P.status);
+            if (!dead) join_copy<4>(slots + ahead.slot * slot_bytes, &full[ahead.slot], src, row);
+            ahead = ahead.next(kJoinBackSlots);
+        }
+    };
     bool in[CH];
     float gw[CH][8], w2[CH][8], a_pre[CH][8] = {};
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         in[k] = c0 + k * apart < cols;
-        for (int i = 0; i < row_units; ++i)
-            if (!in[k] || (!P.dr && i < at_r) || (!P.pre && i >= at_r && i < at_b) || (!P.b && i >= at_b))
-                mine[k * row_units + i] = mine[turn_units + k * row_units + i] = make_uint4(0, 0, 0, 0);
+        join_gains(P.w_pre, nullptr, 0, c0 + k * apart, in[k], w2[k]);
     }
-    const auto fetch = [&](int64_t row, int turn) {
-        const int c = 256 * warp;
-        uint4 *slot = mine - lane * kSlot + turn * turn_units;
-        const int64_t at = row * cols + c;
-        __syncwarp();                                  // (every lane has read what the slots held)
-#pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            if (P.dr) ring_fetch<TX, kSlot>(slot + k * row_units, P.dr, at + k * apart, c + k * apart, cols);
-            if (P.pre) {
-                ring_fetch<TX, kSlot>(slot + k * row_units + at_r, P.r, at + k * apart, c + k * apart, cols);
-                ring_fetch<TB, kSlot>(slot + k * row_units + at_h, P.dh, at + k * apart, c + k * apart, cols);
-            }
-            if (P.b) ring_fetch<TB, kSlot>(slot + k * row_units + at_b, P.b, at + k * apart, c + k * apart, cols);
-        }
-        cp_async_commit();
-    };
-    pdl_wait();
-#pragma unroll
-    for (int k = 0; k < CH; ++k) join_gains(P.w_pre, nullptr, 0, c0 + k * apart, in[k], w2[k]);
     const float factor = P.drop ? P.d.factor : 1.0f;
     int half = 0;
     for (int64_t item = blockIdx.x; item < P.it.gates * P.it.splits; item += gridDim.x) {
         const ItemRows rows = item_rows(P.it, item);
         float S[CH][8] = {};                          // of R dropout' b rstd_post
-        int turn = 0;
-        if (rows.first + sub < rows.end) fetch(rows.first + sub, 0);
-#pragma unroll
-        for (int k = 0; k < CH; ++k) join_gains(P.gate, P.post ? P.w_post : nullptr, rows.gate * cols, c0 + k * apart, in[k], gw[k]);
         float next1 = 1.0f, next2 = 0.0f;             // 1 / RMS of the next row, read a row ahead
         if (rows.first + sub < rows.end) {
             if (P.post) next1 = __ldg(P.rstd_post + rows.first + sub);
             if (P.pre) next2 = __ldg(P.rstd_pre + rows.first + sub);
         }
-        for (int64_t row = rows.first + sub; row < rows.end; row += subs, turn ^= 1) {
-            const uint4 *slot = mine + turn * turn_units;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) join_gains(P.gate, P.post ? P.w_post : nullptr, rows.gate * cols, c0 + k * apart, in[k], gw[k]);
+        if (rows.first + sub < rows.end) fetch(rows.first + sub);
+        for (int64_t row = rows.first + sub; row < rows.end; row += subs) {
+            const int64_t at = row * cols + c0;
             const float rstd1 = next1, rstd2 = next2;
             if (row + subs < rows.end) {
                 if (P.post) next1 = __ldg(P.rstd_post + row + subs);
                 if (P.pre) next2 = __ldg(P.rstd_pre + row + subs);
-                fetch(row + subs, turn ^ 1);
-                cp_async_wait<1>();
-            } else {
-                cp_async_wait<0>();
+                fetch(row + subs);
             }
-            __syncwarp();
-            const int64_t at = row * cols + c0;
+            join_wait(&full[place.slot], place.ph, dead, P.status);
+            const uint8_t *const my_g = slots + place.slot * slot_bytes, *const my_r = my_g + row_x, *const my_h = my_g + off_h, *const my_b = my_g + off_b;
+            const auto get_g = [&](int k, float (&v)[8]) { ring_read<TX>(my_g, c0 + k * apart, in[k] && P.dr, v); };
+            const auto get_r = [&](int k, float (&v)[8]) { ring_read<TX>(my_r, c0 + k * apart, in[k] && P.pre, v); };
+            const auto get_h = [&](int k, float (&v)[8]) { ring_read<TB>(my_h, c0 + k * apart, in[k] && P.pre, v); };
+            const auto get_b = [&](int k, float (&v)[8]) { ring_read<TB>(my_b, c0 + k * apart, in[k] && P.b, v); };
             // Both means from one exchange: the second, of v w_post b, is linear in the first, m, with R = (dr + dh w_pre rstd_pre) - r m.
             float sums[3] = {0.0f, 0.0f, 0.0f};
             uint32_t kept = 0;                        // which elements the dropout keeps, a bit each
+            {
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                float h[8], r[8], g[8], b[8];
-                ring_read<TB>(slot + k * row_units + at_h, h);
-                ring_read<TX>(slot + k * row_units + at_r, r);
-                ring_read<TX>(slot + k * row_units, g);
-                ring_read<TB>(slot + k * row_units + at_b, b);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    a_pre[k][e] = fmaf(h[e] * r[e], rstd2, a_pre[k][e]);
-                    h[e] *= w2[k][e];
-                    sums[0] = fmaf(h[e], r[e], sums[0]);
-                    b[e] *= gw[k][e];
-                }
-                if (P.drop) {
-                    Kept<true> q;
-                    q.make(P.d, keys, P.drop, at - 8 * lane + k * apart, 0);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) { const bool on = q[e]; kept |= on ? 1u << (8 * k + e) : 0u; b[e] = on ? b[e] : 0.0f; }
-                }
-                if (P.post) {
+                for (int k = 0; k < CH; ++k) {
+                    float h[8], r[8], g[8], b[8];
+                    get_h(k, h); get_r(k, r); get_g(k, g); get_b(k, b);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        sums[1] = fmaf(fmaf(h[e], rstd2, g[e]), b[e], sums[1]);
-                        sums[2] = fmaf(r[e], b[e], sums[2]);
+                        a_pre[k][e] = fmaf(h[e] * r[e], rstd2, a_pre[k][e]);
+                        h[e] *= w2[k][e];
+                        sums[0] = fmaf(h[e], r[e], sums[0]);
+                        b[e] *= gw[k][e];
+                    }
+                    if (P.drop) {
+                        Kept<true> q;
+                        q.make(P.d, keys, P.drop, at - 8 * lane + k * apart, 0);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) { const bool on = q[e]; kept |= on ? 1u << (8 * k + e) : 0u; b[e] = on ? b[e] : 0.0f; }
+                    }
+                    if (P.post) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            sums[1] = fmaf(fmaf(h[e], rstd2, g[e]), b[e], sums[1]);
+                            sums[2] = fmaf(r[e], b[e], sums[2]);
+                        }
                     }
                 }
             }
-            if (P.pre || P.post) { group_sums<WARP>(sums, scratch, half); half ^= 1; }
+            if (P.pre || P.post) { group_sums<WARP>(sums, scratch, half, warps); half ^= 1; }
             // R = dr + rstd2 (dh w_pre) - r m2;  db = z rstd1 - b m1 with z = R dropout' gate w_post
             const float m2 = P.pre ? sums[0] * P.inv_cols * rstd2 * rstd2 * rstd2 : 0.0f;
             const float m1 = P.post ? (sums[1] - m2 * sums[2]) * factor * P.inv_cols * rstd1 * rstd1 * rstd1 : 0.0f;
             const float f1 = factor * rstd1;
+            {
 #pragma unroll
-            for (int k = 0; k < CH; ++k) {
-                float R[8];
-                ring_read<TX>(slot + k * row_units, R);
-                if (P.pre) {
-                    float h[8], r[8];
-                    ring_read<TB>(slot + k * row_units + at_h, h);
-                    ring_read<TX>(slot + k * row_units + at_r, r);
+                for (int k = 0; k < CH; ++k) {
+                    float R[8];
+                    get_g(k, R);
+                    if (P.pre) {
+                        float h[8], r[8];
+                        get_h(k, h); get_r(k, r);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) R[e] = fmaf(-r[e], m2, fmaf(h[e] * w2[k][e], rstd2, R[e]));
-                }
-                if (P.b) {
-                    float b[8], z[8];
-                    ring_read<TB>(slot + k * row_units + at_b, b);
+                        for (int e = 0; e < 8; ++e) R[e] = fmaf(-r[e], m2, fmaf(h[e] * w2[k][e], rstd2, R[e]));
+                    }
+                    if (P.b) {
+                        float b[8], z[8];
+                        get_b(k, b);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] = R[e] * f1;
-                    if (P.drop) {
+                        for (int e = 0; e < 8; ++e) z[e] = R[e] * f1;
+                        if (P.drop) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const bool on = (kept >> (8 * k + e)) & 1u;
-                            z[e] = on ? z[e] : 0.0f;
-                            S[k][e] = on ? fmaf(z[e], b[e], S[k][e]) : S[k][e];
+                            for (int e = 0; e < 8; ++e) {
+                                const bool on = (kept >> (8 * k + e)) & 1u;
+                                z[e] = on ? z[e] : 0.0f;
+                                S[k][e] = on ? fmaf(z[e], b[e], S[k][e]) : S[k][e];
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) S[k][e] = fmaf(z[e], b[e], S[k][e]);
                         }
-                    } else {
+                        if (P.db && in[k]) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) S[k][e] = fmaf(z[e], b[e], S[k][e]);
+                            for (int e = 0; e < 8; ++e) z[e] = P.post ? fmaf(-b[e], m1, z[e] * gw[k][e]) : z[e] * gw[k][e];
+                            put_vec(P.db, at + k * apart, pack8<TB>(z), P.wide);
+                        }
                     }
-                    if (P.db && in[k]) {
+                    if (P.dx && in[k]) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) z[e] = P.post ? fmaf(-b[e], m1, z[e] * gw[k][e]) : z[e] * gw[k][e];
-                        put_vec(P.db, at + k * apart, pack8<TB>(z), P.wide);
+                        for (int e = 0; e < 8; ++e) R[e] *= P.alpha;
+                        put_vec(P.dx, at + k * apart, pack8<TX>(R), P.wide);
                     }
-                }
-                if (P.dx && in[k]) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) R[e] *= P.alpha;
-                    put_vec(P.dx, at + k * apart, pack8<TX>(R), P.wide);
                 }
             }
+            __syncwarp();
+            if (!WARP && lane == 0) mbar_arrive(&bars.empty[place.slot]);
+            place = place.next(kJoinBackSlots);
         }
-        if (P.sum_gate) join_leave<CH, WARP, true>(S, P.part_gate + item * cols, P.post ? P.w_post : nullptr, cols, c0, apart, false, fold);
-        if (P.sum_post) join_leave<CH, WARP, true>(S, P.part_post + (int64_t)blockIdx.x * cols, P.gate ? P.gate + rows.gate * cols : nullptr, cols, c0, apart, item != blockIdx.x, fold);
+        if (P.sum_gate) join_leave<CH, WARP, true>(S, P.part_gate + item * cols, P.post ? P.w_post : nullptr, cols, c0, apart, false, fold, 32 * all_warps);
+        if (P.sum_post)
+            join_leave<CH, WARP, true>(S, P.part_post + (int64_t)blockIdx.x * cols, P.gate ? P.gate + rows.gate * cols : nullptr, cols, c0, apart, item != blockIdx.x, fold, 32 * all_warps);
     }
-    if (P.sum_pre) join_leave<CH, WARP, true>(a_pre, P.part_pre + (int64_t)blockIdx.x * cols, nullptr, cols, c0, apart, false, fold);
+    if (P.sum_pre) join_leave<CH, WARP, true>(a_pre, P.part_pre + (int64_t)blockIdx.x * cols, nullptr, cols, c0, apart, false, fold, 32 * all_warps);
 }
 
 // ---- any rows -------------------------------------------------------------------------------------------------------------
@@ -556,6 +580,7 @@ join_fwd_any_kernel(const __grid_constant__ JoinParams P, const __grid_constant_
         }
     };
     pdl_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;           // (nothing here waits)
     for (int64_t item = blockIdx.x; item < P.it.gates * P.it.splits; item += gridDim.x) {
         const ItemRows rows = item_rows(P.it, item);
         JoinRow<TX, TB, CH> R;
@@ -574,7 +599,7 @@ join_fwd_any_kernel(const __grid_constant__ JoinParams P, const __grid_constant_
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
                 }
-                rstd = rsqrtf(group_sum<WARP>(s, scratch, 0) * P.inv_cols + P.eps);
+                rstd = rsqrtf(group_sum<WARP>(s, scratch, 0, warps) * P.inv_cols + P.eps);
                 if (P.rstd_post && warp == 0 && lane == 0) P.rstd_post[row] = rstd;
             }
             float s2 = 0.0f, r8[CH][8];
@@ -608,7 +633,7 @@ join_fwd_any_kernel(const __grid_constant__ JoinParams P, const __grid_constant_
                 for (int e = 0; e < 8; ++e) s2 = fmaf(r8[k][e], r8[k][e], s2);      // (zero behind the last column, as x and b are)
             }
             if (P.pre) {
-                const float rstd2 = rsqrtf(group_sum<WARP>(s2, scratch, 1) * P.inv_cols + P.eps);
+                const float rstd2 = rsqrtf(group_sum<WARP>(s2, scratch, 1, warps) * P.inv_cols + P.eps);
                 if (P.rstd_pre && warp == 0 && lane == 0) P.rstd_pre[row] = rstd2;
 #pragma unroll
                 for (int k = 0; k < CH; ++k) {
@@ -647,6 +672,7 @@ join_bwd_any_kernel(const __grid_constant__ JoinBwdParams P, const __grid_consta
     };
     float a_pre[CH][8] = {};
     pdl_wait();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;           // (nothing here waits)
     for (int64_t item = blockIdx.x; item < P.it.gates * P.it.splits; item += gridDim.x) {
         const ItemRows rows = item_rows(P.it, item);
         float S[CH][8] = {};
@@ -674,7 +700,7 @@ join_bwd_any_kernel(const __grid_constant__ JoinBwdParams P, const __grid_consta
                         s = fmaf(t, w[e], s);
                     }
                 }
-                mean2 = group_sum<WARP>(s, scratch, 0) * P.inv_cols;
+                mean2 = group_sum<WARP>(s, scratch, 0, warps) * P.inv_cols;
             }
             float s1 = 0.0f, z[CH][8];                   // z = R dropout' gate w_post
 #pragma unroll
@@ -720,7 +746,7 @@ join_bwd_any_kernel(const __grid_constant__ JoinBwdParams P, const __grid_consta
                 }
             }
             if (P.b) {
-                const float mean1 = P.post ? group_sum<WARP>(s1, scratch, 1) * P.inv_cols * rstd1 : 0.0f;
+                const float mean1 = P.post ? group_sum<WARP>(s1, scratch, 1, warps) * P.inv_cols * rstd1 : 0.0f;
                 if (P.db) {
 #pragma unroll
                     for (int k = 0; k < CH; ++k) {
@@ -736,12 +762,12 @@ join_bwd_any_kernel(const __grid_constant__ JoinBwdParams P, const __grid_consta
             }
             end_row<WARP>(P.pre, P.post);
         }
-        if (P.sum_gate) join_leave<CH, WARP, VEC>(S, P.part_gate + item * (int64_t)cols, P.post ? P.w_post : nullptr, cols, col(0), 256 * warps, false, fold);
+        if (P.sum_gate) join_leave<CH, WARP, VEC>(S, P.part_gate + item * (int64_t)cols, P.post ? P.w_post : nullptr, cols, col(0), 256 * warps, false, fold, (int)blockDim.x);
         if (P.sum_post)
             join_leave<CH, WARP, VEC>(S, P.part_post + (int64_t)blockIdx.x * cols, P.gate ? P.gate + rows.gate * (int64_t)cols : nullptr, cols, col(0), 256 * warps,
-                                      item != blockIdx.x, fold);
+                                      item != blockIdx.x, fold, (int)blockDim.x);
     }
-    if (P.sum_pre) join_leave<CH, WARP, VEC>(a_pre, P.part_pre + (int64_t)blockIdx.x * cols, nullptr, cols, col(0), 256 * warps, false, fold);
+    if (P.sum_pre) join_leave<CH, WARP, VEC>(a_pre, P.part_pre + (int64_t)blockIdx.x * cols, nullptr, cols, col(0), 256 * warps, false, fold, (int)blockDim.x);
 }
 #endif
 
@@ -782,12 +808,12 @@ __global__ void __launch_bounds__(32 * kSumHigh) join_sum_kernel(const __grid_co
 
 // ================================================================= host side
 struct JoinShape { int ch, threads; bool warp; };
-constexpr size_t kJoinMaxRing = 224 * 1024, kJoinSmRings = 222 * 1024;        // of a block, of an SM
-// Shared memory of a block's ring: three rows forward, with one tensor of each type, and two backwards, with two.
+constexpr size_t kJoinMaxRing = 200 * 1024, kJoinSmRings = 222 * 1024;        // of a block, of an SM
+// Shared memory of a block's ring: forward slots of one tensor of each type, backwards of two.
 static size_t join_ring(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
 {
-    const size_t pieces = (size_t)s.ch * tensors * (dtype_size(d->x_dtype) + dtype_size(d->b_dtype)) / 2;
-    return (tensors == 1 ? 3 : 2) * 16 * (pieces | 1) * (size_t)s.threads;
+    const size_t slots = tensors == 1 ? kJoinSlots : kJoinBackSlots;
+    return slots * (size_t)(s.warp ? kJoinWarpRows : 1) * (size_t)d->cols * (size_t)tensors * (dtype_size(d->x_dtype) + dtype_size(d->b_dtype));
 }
 // A thread takes sixteen columns, eight where the rings of two blocks would not fit an SM, and 32 (without a ring) beyond 8192.
 static JoinShape join_shape(const qbp_resnorm_desc *d, int tensors)
@@ -802,12 +828,13 @@ static JoinShape join_shape(const qbp_resnorm_desc *d, int tensors)
 }
 
 // Runs `call` with the kernel's compile-time choices for rows that are read in vectors.
-#define QBP_FOR_JOIN(shape, CH, WARP, call)                                                                                   \
+#define QBP_FOR_JOIN(shape, CH, WARP, MAXT, call)                                                                             \
     do {                                                                                                                      \
-        if ((shape).warp && (shape).ch == 1) { constexpr int CH = 1; constexpr bool WARP = true; call; }                      \
-        else if ((shape).warp) { constexpr int CH = 2; constexpr bool WARP = true; call; }                                    \
-        else if ((shape).ch == 1) { constexpr int CH = 1; constexpr bool WARP = false; call; }                                \
-        else { constexpr int CH = 2; constexpr bool WARP = false; call; }                                                     \
+        if ((shape).warp && (shape).ch == 1) { constexpr int CH = 1, MAXT = 256; constexpr bool WARP = true; call; }          \
+        else if ((shape).warp) { constexpr int CH = 2, MAXT = 256; constexpr bool WARP = true; call; }                        \
+        else if ((shape).ch == 1) { constexpr int CH = 1, MAXT = 512; constexpr bool WARP = false; call; }                    \
+        else if ((shape).threads <= 256) { constexpr int CH = 2, MAXT = 256; constexpr bool WARP = false; call; }             \
+        else { constexpr int CH = 2, MAXT = 512; constexpr bool WARP = false; call; }                                         \
     } while (0)
 
 // Launches with the ring's shared memory.
@@ -815,7 +842,7 @@ template <typename Params>
 static int launch_join(void (*kernel)(Params, PhiloxKeys), PerDeviceOnce &once, int64_t blocks, const JoinShape &s, size_t smem, cudaStream_t st, const Params &P,
                        const PhiloxKeys &keys)
 {
-    if (smem > 24 * 1024) QBP_SMEM_OPT_IN(once, kernel, s.warp ? (size_t)200 * 1024 : kJoinMaxRing);       // (with the static arrays beside it, over 48 KB)
+    if (smem > 24 * 1024) QBP_SMEM_OPT_IN(once, kernel, kJoinMaxRing);       // (with the static arrays beside it, over 48 KB)
     launch(kernel, dim3((unsigned)blocks), s.threads, smem, st, P, keys);
     return QBP_OK;
 }
@@ -855,18 +882,18 @@ static JoinCut join_cut(const qbp_resnorm_desc *d, const JoinShape &s, bool per_
 // Blocks of a wave: 16 warps an SM (8 backwards where a row is a warp's), which their registers allow, or what their rings leave room for.
 static int64_t join_blocks(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
 {
-    const int64_t per_sm = std::min<int64_t>((s.warp && tensors == 2 ? 256 : 512) / s.threads, (int64_t)(227 * 1024 / (join_ring(d, s, tensors) + 2048 + (s.warp ? 16384 : 0))));
+    const int64_t per_sm = s.ch > 2 ? 1 : std::min<int64_t>((s.warp && tensors == 2 ? 256 : 512) / s.threads, (int64_t)(227 * 1024 / (join_ring(d, s, tensors) + 2048 + (s.warp && tensors == 2 ? 16384 : 0))));
     return (int64_t)sm_count() * std::max<int64_t>(per_sm, 1);
 }
 static JoinCut join_cut_bwd(const qbp_resnorm_desc *d, bool per_gate)
 {
     const JoinShape s = join_shape(d, 2);
-    return join_cut(d, s, per_gate, join_blocks(d, s, 2), 4);
+    return join_cut(d, s, per_gate, join_blocks(d, s, 2), s.warp ? 2 : 4);
 }
 
 extern "C" __attribute__((visibility("default"))) int qbp_resnorm_fwd(const qbp_resnorm_desc *d, const void *x, const void *b, const float *w_post,
                                                                       const float *gate, const float *w_pre, void *r, void *h, float *rstd_post,
-                                                                      float *rstd_pre, void *stream)
+                                                                      float *rstd_pre, void *ws, size_t ws_bytes, void *stream)
 {
     cudaStream_t st = (cudaStream_t)stream;
     int rc = check_join(d, "resnorm_fwd", b, gate, w_post, w_pre);
@@ -876,6 +903,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_fwd(const qbp_
         return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: a tensor is NULL or misaligned");
     if (!r && (b || d->alpha != 1.0f)) return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: r may be NULL only where it is x");
     if (!r && !d->pre) return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: no output wanted");
+    if (!ws || !aligned_to(ws, 256) || ws_bytes < 256) return fail(QBP_ERR_WORKSPACE, "resnorm_fwd: workspace NULL, misaligned or smaller than 256 bytes");
     JoinParams P{};
     const JoinShape s = join_shape(d, 1);
     const JoinCut c = join_cut(d, s, gate != nullptr, join_blocks(d, s, 1), 1);
@@ -885,21 +913,22 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_fwd(const qbp_
     P.post = d->post ? 1 : 0; P.pre = d->pre ? 1 : 0; P.x_dtype = d->x_dtype; P.b_dtype = d->b_dtype;
     P.d = dropout_params(d->p, d->tensor_id, d->index_base);
     P.drop = P.d.threshold == 65536u ? 2 : P.d.threshold ? 1 : 0;
+    P.status = static_cast<int *>(ws);
     P.wide = aligned_to(r, 32) && aligned_to(h, 32) ? 1 : 0;
     const PhiloxKeys keys = philox_keys_host(d->seed);
     const bool vec = d->cols % 8 == 0 && aligned16(x) && aligned16(b) && aligned16(r) && aligned16(h) && aligned16(w_post) && aligned16(gate) && aligned16(w_pre);
     QBP_TRACE_BEGIN(st);
     if (vec && s.ch <= 2)
-        QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, CH, WARP, {
+        QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, CH, WARP, MAXT, {
             static PerDeviceOnce once;
-            if ((rc = launch_join(join_fwd_kernel<TX, TB, CH, WARP>, once, c.blocks, s, join_ring(d, s, 1), st, P, keys))) return rc;
+            if ((rc = launch_join(join_fwd_kernel<TX, TB, CH, WARP, MAXT>, once, c.blocks, s, join_ring(d, s, 1), st, P, keys))) return rc;
         })));
     else if (vec)
         QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, (launch(join_fwd_any_kernel<TX, TB, 4, false, true>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys))));
     else if (s.ch == 4)
         launch(join_fwd_any_kernel<AnyReal, AnyReal, 4, false, false>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys);
     else
-        QBP_FOR_JOIN(s, CH, WARP, (launch(join_fwd_any_kernel<AnyReal, AnyReal, CH, WARP, false>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys)));
+        QBP_FOR_JOIN(s, CH, WARP, MAXT, (launch(join_fwd_any_kernel<AnyReal, AnyReal, CH, WARP, false>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys)));
     QBP_LAUNCH_OK("join_fwd_kernel");
     return QBP_OK;
 }
@@ -945,6 +974,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
     const int64_t items = c.it.gates * c.it.splits;
     WsCarver w(ws, ws_bytes);
     JoinBwdParams P{};
+    P.status = w.take<int>(1);
     P.it = c.it;
     P.dr = dr; P.dh = dh; P.b = b; P.r = r; P.rstd_post = rstd_post; P.rstd_pre = rstd_pre; P.w_post = w_post; P.gate = gate; P.w_pre = w_pre;
     P.dx = dx; P.db = db; P.alpha = d->alpha; P.inv_cols = (float)(1.0 / (double)d->cols);
@@ -964,16 +994,16 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
                      aligned16(gate) && aligned16(w_pre);
     QBP_TRACE_BEGIN(st);
     if (vec && s.ch <= 2)
-        QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, CH, WARP, {
+        QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, CH, WARP, MAXT, {
             static PerDeviceOnce once;
-            if ((rc = launch_join(join_bwd_kernel<TX, TB, CH, WARP>, once, c.blocks, s, join_ring(d, s, 2), st, P, keys))) return rc;
+            if ((rc = launch_join(join_bwd_kernel<TX, TB, CH, WARP, MAXT>, once, c.blocks, s, join_ring(d, s, 2), st, P, keys))) return rc;
         })));
     else if (vec)
         QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, (launch(join_bwd_any_kernel<TX, TB, 4, false, true>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys))));
     else if (s.ch == 4)
         launch(join_bwd_any_kernel<AnyReal, AnyReal, 4, false, false>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys);
     else
-        QBP_FOR_JOIN(s, CH, WARP, (launch(join_bwd_any_kernel<AnyReal, AnyReal, CH, WARP, false>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys)));
+        QBP_FOR_JOIN(s, CH, WARP, MAXT, (launch(join_bwd_any_kernel<AnyReal, AnyReal, CH, WARP, false>, dim3((unsigned)c.blocks), s.threads, 0, st, P, keys)));
     QBP_LAUNCH_OK("join_bwd_kernel");
     JoinSums S{};
     int jobs = 0;

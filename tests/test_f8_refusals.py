@@ -67,8 +67,8 @@ def desc(B, **change):
     return B.ResnormDesc(**{**d, **change})
 
 
-def fwd(B, d, x=P, b=P, w1=P, gate=P, w2=P, r=P, h=P, q1=P, q2=P):
-    return B.lib.qbp_resnorm_fwd(C.addressof(d) if d else None, x, b, w1, gate, w2, r, h, q1, q2, None)
+def fwd(B, d, x=P, b=P, w1=P, gate=P, w2=P, r=P, h=P, q1=P, q2=P, ws=P, n=BIG):
+    return B.lib.qbp_resnorm_fwd(C.addressof(d) if d else None, x, b, w1, gate, w2, r, h, q1, q2, ws, n, None)
 
 
 def bwd(B, d, dr=P, dh=P, b=P, r=P, q1=P, q2=P, w1=P, gate=P, w2=P, dx=P, db=P, dw1=P, dg=P, dw2=P, ws=P, n=BIG):
@@ -86,6 +86,7 @@ def test_joins(B):
     assert fwd(B, desc(B, cols=B.QBP_RESNORM_MAX_COLS + 1)) == -2
     for kw in (dict(x=None), dict(x=P + 2), dict(b=P + 1), dict(h=None), dict(h=P + 1), dict(r=None), dict(w1=P + 2), dict(gate=P + 1)):
         assert fwd(B, desc(B), **kw) == -1, kw
+    assert fwd(B, desc(B), ws=None) == -4 and fwd(B, desc(B), n=128) == -4 and fwd(B, desc(B), ws=P + 4) == -4
     # without a block output: no norm after it, gate or dropout; r may be left out where it is x
     assert fwd(B, desc(B), b=None) == -1 and fwd(B, desc(B, post=0), b=None) == -1 and fwd(B, desc(B, post=0, p=0.5), b=None, gate=None) == -1
     assert fwd(B, desc(B, post=0, alpha=0.5), b=None, gate=None, r=None) == -1 and fwd(B, desc(B, post=0, pre=0), b=None, gate=None, r=None) == -1
