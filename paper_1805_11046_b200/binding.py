@@ -473,11 +473,11 @@ def _here(*tensors) -> int:
 
 
 def _new(shape, dtype, index):
-    """An uncleared tensor on a device, made from an empty one of its type: without arguments for type and device the allocation
-    takes 1.4 us of the host's time instead of 2.4."""
+    """An uncleared tensor on a device (shape: an int or a tuple), made from an empty one of its type: without arguments for type and
+    device the allocation takes 1.0 us of the host's time instead of 2.4."""
     t = _EMPTY.get((dtype, index))
     if t is None: t = _EMPTY[dtype, index] = torch.empty(0, dtype=dtype, device=torch.device("cuda", index))
-    return t.new_empty(shape)
+    return t.new(shape) if shape.__class__ is int else t.new(*shape)
 
 
 def _scratch(nbytes, index):
@@ -609,9 +609,10 @@ def resnorm_desc(x, b=None, alpha=1.0, eps=1e-6, gate_rows=0, p=0.0, seed=0, ten
 
 
 def _real(t, count, dtype, name):
-    """Device address of a dense real-valued tensor of `count` elements and this qbp_dtype (None: NULL)."""
+    """Device address of a dense real-valued tensor of `count` elements and this type (None: NULL)."""
     if t is None: return None
-    if _DTYPES.get(t.dtype) != dtype: raise TypeError(f"{name}: {t.dtype} is not the descriptor's type")
+    if t.dtype is dtype and t.numel() == count and t.is_contiguous(): return t.data_ptr()
+    if t.dtype is not dtype: raise TypeError(f"{name}: {t.dtype}, {dtype} is wanted")
     if t.numel() != count: raise ValueError(f"{name}: {t.numel()} elements, {count} are wanted")
     return _addr(t)
 
@@ -624,18 +625,18 @@ def qbp_resnorm_fwd(d: ResnormDesc, x, b=None, w_post=None, gate=None, w_pre=Non
     """Returns (r, h, rstd_post, rstd_pre), None where there is none: r without a block output and alpha 1 is x itself, h and its
     rstd without a norm before the next block.  h has b's type (without b, the descriptor's)."""
     device = _here(x, b, w_post, gate, w_pre, r, h, rstd_post, rstd_pre, ws)
-    rows, cols, xt, bt = d.rows, d.cols, d.x_dtype, d.b_dtype
+    rows, cols, xt, bt, f32 = d.rows, d.cols, _REALS[d.x_dtype], _REALS[d.b_dtype], torch.float32
     n = rows * cols
     if r is None and not (b is None and d.alpha == 1.0): r = torch.empty_like(x)
     if d.pre:
-        if h is None: h = torch.empty_like(b) if b is not None else _new(x.shape, _REALS[bt], device)
-        if rstd_pre is None: rstd_pre = _new(rows, torch.float32, device)
-    if d.post and rstd_post is None: rstd_post = _new(rows, torch.float32, device)
+        if h is None: h = torch.empty_like(b) if b is not None else _new(x.shape, bt, device)
+        if rstd_pre is None: rstd_pre = _new(rows, f32, device)
+    if d.post and rstd_post is None: rstd_post = _new(rows, f32, device)
     if ws is None: ws = _scratch(256, device)
-    _check(lib.qbp_resnorm_fwd(C.addressof(d), _real(x, n, xt, "x"), _real(b, n, bt, "b"), _real(w_post, cols, QBP_F32, "w_post"),
-                               _real(gate, _gates(d) * cols, QBP_F32, "gate"), _real(w_pre, cols, QBP_F32, "w_pre"),
-                               _real(r, n, xt, "r"), _real(h, n, bt, "h"), _real(rstd_post, rows, QBP_F32, "rstd_post"),
-                               _real(rstd_pre, rows, QBP_F32, "rstd_pre"), ws.data_ptr(), ws.numel(), _stream_handle(device)))
+    _check(lib.qbp_resnorm_fwd(C.addressof(d), _real(x, n, xt, "x"), _real(b, n, bt, "b"), _real(w_post, cols, f32, "w_post"),
+                               _real(gate, _gates(d) * cols, f32, "gate"), _real(w_pre, cols, f32, "w_pre"),
+                               _real(r, n, xt, "r"), _real(h, n, bt, "h"), _real(rstd_post, rows, f32, "rstd_post"),
+                               _real(rstd_pre, rows, f32, "rstd_pre"), ws.data_ptr(), ws.numel(), _stream_handle(device)))
     return r, h, rstd_post, rstd_pre
 
 
@@ -644,18 +645,18 @@ def qbp_resnorm_bwd(d: ResnormDesc, dr, dh, b, r, rstd_post, rstd_pre, w_post=No
     """The gradients (dx, db, dw_post, dgate, dw_pre) from dr (None: nothing else uses r) and dh.  Gradients of what the forward
     did not have are None; want_params=False: dx and db alone."""
     device = _here(dr, dh, b, r, rstd_post, rstd_pre, w_post, gate, w_pre, dx, db, ws)
-    rows, cols, xt, bt = d.rows, d.cols, d.x_dtype, d.b_dtype
+    rows, cols, xt, bt, f32 = d.rows, d.cols, _REALS[d.x_dtype], _REALS[d.b_dtype], torch.float32
     n, like = rows * cols, dr if dr is not None else r
     if dx is None: dx = torch.empty_like(like)
     if db is None and b is not None: db = torch.empty_like(b)
-    dw1 = _new(cols, torch.float32, device) if want_params and d.post else None
+    dw1 = _new(cols, f32, device) if want_params and d.post else None
     dg = _new((_gates(d), cols), torch.float32, device) if want_params and gate is not None else None
-    dw2 = _new(cols, torch.float32, device) if want_params and d.pre else None
+    dw2 = _new(cols, f32, device) if want_params and d.pre else None
     if ws is None: ws = _scratch(lib.qbp_resnorm_bwd_workspace_bytes(C.addressof(d)), device)
     _check(lib.qbp_resnorm_bwd(C.addressof(d), _real(dr, n, xt, "dr"), _real(dh, n, bt, "dh"), _real(b, n, bt, "b"),
-                               _real(r, n, xt, "r"), _real(rstd_post, rows, QBP_F32, "rstd_post"), _real(rstd_pre, rows, QBP_F32, "rstd_pre"),
-                               _real(w_post, cols, QBP_F32, "w_post"), _real(gate, _gates(d) * cols, QBP_F32, "gate"),
-                               _real(w_pre, cols, QBP_F32, "w_pre"), _real(dx, n, xt, "dx"), _real(db, n, bt, "db"),
+                               _real(r, n, xt, "r"), _real(rstd_post, rows, f32, "rstd_post"), _real(rstd_pre, rows, f32, "rstd_pre"),
+                               _real(w_post, cols, f32, "w_post"), _real(gate, _gates(d) * cols, f32, "gate"),
+                               _real(w_pre, cols, f32, "w_pre"), _real(dx, n, xt, "dx"), _real(db, n, bt, "db"),
                                _addr(dw1), _addr(dg), _addr(dw2), ws.data_ptr(), ws.numel(), _stream_handle(device)))
     return dx, db, dw1, dg, dw2
 

@@ -138,9 +138,11 @@ def test_tensors_of_another_device_and_type(B, monkeypatch):
     with pytest.raises(ValueError, match="scales of"):
         B._scales_fit(torch.zeros(511, dtype=torch.uint8), 128, 512, "sA")
     with pytest.raises(ValueError, match="elements"):
-        B._real(torch.zeros(5), 4, B.QBP_F32, "x")
-    with pytest.raises(TypeError, match="descriptor"):
-        B._real(torch.zeros(4), 4, B.QBP_BF16, "x")
+        B._real(torch.zeros(5), 4, torch.float32, "x")
+    with pytest.raises(TypeError, match="bfloat16 is wanted"):
+        B._real(torch.zeros(4), 4, torch.bfloat16, "x")
+    with pytest.raises(ValueError, match="dense"):
+        B._real(torch.zeros(2, 4).t(), 8, torch.float32, "x")
 
 
 def test_structs_match_the_header(B):
