@@ -579,6 +579,10 @@ def qbp_gemm_f8(A, sA, B, sB, transA=False, transB=False, formatA=QBP_E4M3, form
     return out
 
 
+def qbp_linear_f8_workspace_bytes(M: int, N: int, K: int) -> int:
+    return lib.qbp_linear_f8_workspace_bytes(M, N, K)
+
+
 def qbp_linear_f8(x, w, sw, w_format=QBP_E4M3, y=None, ws=None):
     """y = x w^T of a layer that serves: x [..., K] real-valued, w [N, K] codes and sw their scales over N by K.  y has x's type."""
     device = _here(x, w, sw, y, ws)
@@ -638,6 +642,10 @@ def qbp_resnorm_fwd(d: ResnormDesc, x, b=None, w_post=None, gate=None, w_pre=Non
                                _real(r, n, xt, "r"), _real(h, n, bt, "h"), _real(rstd_post, rows, f32, "rstd_post"),
                                _real(rstd_pre, rows, f32, "rstd_pre"), ws.data_ptr(), ws.numel(), _stream_handle(device)))
     return r, h, rstd_post, rstd_pre
+
+
+def qbp_resnorm_bwd_workspace_bytes(d: ResnormDesc) -> int:
+    return lib.qbp_resnorm_bwd_workspace_bytes(C.addressof(d))
 
 
 def qbp_resnorm_bwd(d: ResnormDesc, dr, dh, b, r, rstd_post, rstd_pre, w_post=None, gate=None, w_pre=None, dx=None, db=None,

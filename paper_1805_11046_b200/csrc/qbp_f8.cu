@@ -333,7 +333,7 @@ template <typename TX> struct SplitRows { static constexpr bool quantise = true;
 template <> struct SplitRows<FromCodes> { static constexpr bool quantise = false; using type = float; };
 
 template <typename TX>
-__global__ void __launch_bounds__(kSplitThreads, 1) f8_split_kernel(const __grid_constant__ F8SplitParams P)
+__global__ void __launch_bounds__(kSplitThreads, 2) f8_split_kernel(const __grid_constant__ F8SplitParams P)
 {
     constexpr bool kQuantise = SplitRows<TX>::quantise;
     using T = typename SplitRows<TX>::type;
@@ -538,6 +538,8 @@ static int launch_f8_split(const F8Product &p, const SplitInput &in, cudaStream_
     P.stage_bytes = (uint32_t)align_up(P.u.tile_bytes + P.v.tile_bytes + 2u * kF8Piece, 1024);
     const uint32_t sums_bytes = P.parts > 1 ? (uint32_t)P.bn * 512u : 0u;
     P.stages = (int)std::min<int64_t>(kSplitMaxStages, (kSplitSmem - 1024 - sums_bytes) / P.stage_bytes);
+    // more than a wave: two CTAs an SM, one's loads beside the other's epilogue
+    if (tiles_n * tiles_m > sm_count()) P.stages = std::min<int>(P.stages, (int)((kSplitSmem / 2 - 2048) / P.stage_bytes));
     P.stages = std::min(P.stages, std::max(2, (P.k_blocks + P.parts - 1) / P.parts + 1));
     P.stages -= P.stages % (int)kSplitRelease;
     static_assert(kSplitMaxStages + (int)kSplitRelease <= 4 * kSplitSets - 3 && kSplitMaxStages + (int)kSplitRelease < kSplitBlockSets &&
@@ -614,10 +616,11 @@ extern "C" __attribute__((visibility("default"))) int qbp_quantize_f8_square(con
 // Whether the product runs on single CTAs.
 // One wave of tiles of 128 on single CTAs against tiles of 256 rows on pairs (one call of many in a row, split and pair, us): 64 x 4096 x
 // 8192 15.7 and 27.3, 512 x 4096 x 512 9.9 and 11.5, 1111 x 2048 x 8192 27.6 and 31.0; two waves: 512 x 8192 x 2048 26.3 and 17.4.
+// Few rows are always theirs, whose half of the MMA is as narrow as they are: 1 x 32768 x 4096 28.6 and 44.1.
 static bool one_wave(const F8Product &p)
 {
     const int64_t rows = p.transA || p.M > 64 ? 128 : 64;
-    return f8_blocks(p.N) * ((p.M + rows - 1) / rows) <= sm_count();
+    return f8_blocks(p.N) * ((p.M + rows - 1) / rows) <= sm_count() || (!p.transA && p.M <= 128);
 }
 static int run_product(const F8Product &p, cudaStream_t st) { return one_wave(p) ? launch_f8_split(p, SplitInput{nullptr, 0}, st) : launch_f8_pair(p, st); }
 

@@ -901,6 +901,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_fwd(const qbp_
     if (d->rows == 0 || d->cols == 0) return QBP_OK;
     if (!real_ok(x, d->x_dtype) || (b && !real_ok(b, d->b_dtype)) || (r && !real_ok(r, d->x_dtype)) || (d->pre && !real_ok(h, d->b_dtype)))
         return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: a tensor is NULL or misaligned");
+    if (!aligned_to(rstd_post, 4) || !aligned_to(rstd_pre, 4)) return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: misaligned fp32 tensors");
     if (!r && (b || d->alpha != 1.0f)) return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: r may be NULL only where it is x");
     if (!r && !d->pre) return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: no output wanted");
     if (!ws || !aligned_to(ws, 256) || ws_bytes < 256) return fail(QBP_ERR_WORKSPACE, "resnorm_fwd: workspace NULL, misaligned or smaller than 256 bytes");

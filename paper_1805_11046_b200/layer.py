@@ -193,7 +193,7 @@ class F8Linear:
 
     def __init__(self, w, grad_format=B.QBP_E4M3):
         self.w, self.grad_format = w, grad_format
-        self.ws = torch.empty(256, dtype=torch.uint8, device=w.device)
+        self.ws = torch.empty(256, dtype=torch.uint8, device=w.device)          # of its own: a captured step keeps its address
         self.codes = self.saved = self.dw = None
 
     def quantise(self):
@@ -204,7 +204,9 @@ class F8Linear:
     def serve(self, x):
         """y for an activation of any number of rows, from the codes quantise() left."""
         q, s, _ = self.codes
-        return B.qbp_linear_f8(x, q, s)
+        need = B.qbp_linear_f8_workspace_bytes(x.numel() // max(x.shape[-1], 1), *q.shape)
+        if self.ws.numel() < need: self.ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+        return B.qbp_linear_f8(x, q, s, ws=self.ws)
 
     def forward(self, x):
         q, s, _ = self.quantise()
@@ -241,18 +243,21 @@ class F8ResidualStack:
         self.step = 0
         self.velocity = None
         self.saved = self.grads = None
+        self.ws = torch.empty(256, dtype=torch.uint8, device=dev)               # of the joins
 
     def forward(self, x, h_dtype=torch.bfloat16):
         """x [rows, C]: the residual stream, of its own type.  Returns the last block's h (h_dtype)."""
         n = len(self.linears)
         first = B.resnorm_desc(x, eps=self.eps, h_dtype=h_dtype)
-        _, h, _, q = B.qbp_resnorm_fwd(first, x, w_pre=self.w_first)
+        need = B.qbp_resnorm_bwd_workspace_bytes(first)
+        if self.ws.numel() < need: self.ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+        _, h, _, q = B.qbp_resnorm_fwd(first, x, w_pre=self.w_first, ws=self.ws)
         joins, r = [], x
         for i, lin in enumerate(self.linears):
             b = lin.forward(h)
             # (a stream of draws for each block and step)
             d = B.resnorm_desc(r, b, alpha=self.alpha, eps=self.eps, p=self.p, seed=self.seed, tensor_id=self.step * n + i)
-            r, h, q1, q2 = B.qbp_resnorm_fwd(d, r, b, self.w_post[i], self.gate[i], self.w_pre[i])
+            r, h, q1, q2 = B.qbp_resnorm_fwd(d, r, b, self.w_post[i], self.gate[i], self.w_pre[i], ws=self.ws)
             joins.append((d, b, r, q1, q2))
         self.saved = (first, x, q, joins)
         return h
@@ -263,10 +268,10 @@ class F8ResidualStack:
         dr, grads = None, []
         for i in reversed(range(len(joins))):
             d, b, r, q1, q2 = joins[i]
-            dr, db, dw1, dg, dw2 = B.qbp_resnorm_bwd(d, dr, dh, b, r, q1, q2, self.w_post[i], self.gate[i], self.w_pre[i])
+            dr, db, dw1, dg, dw2 = B.qbp_resnorm_bwd(d, dr, dh, b, r, q1, q2, self.w_post[i], self.gate[i], self.w_pre[i], ws=self.ws)
             dh = self.linears[i].backward(db)
             grads.append((self.linears[i].dw, dw1, dg.view(-1), dw2))
-        dx, _, _, _, dw = B.qbp_resnorm_bwd(first, dr, dh, None, x, None, q, w_pre=self.w_first)
+        dx, _, _, _, dw = B.qbp_resnorm_bwd(first, dr, dh, None, x, None, q, w_pre=self.w_first, ws=self.ws)
         self.grads = (grads[::-1], dw)
         return dx
 
@@ -280,4 +285,4 @@ class F8ResidualStack:
         self.step += 1
 
     def status(self) -> int:
-        return min(lin.status() for lin in self.linears)
+        return min([B.status_word(self.ws)] + [lin.status() for lin in self.linears])

@@ -84,7 +84,7 @@ def test_join_descriptors(B, change):
 
 def test_joins(B):
     assert fwd(B, desc(B, cols=B.QBP_RESNORM_MAX_COLS + 1)) == -2
-    for kw in (dict(x=None), dict(x=P + 2), dict(b=P + 1), dict(h=None), dict(h=P + 1), dict(r=None), dict(w1=P + 2), dict(gate=P + 1)):
+    for kw in (dict(x=None), dict(x=P + 2), dict(b=P + 1), dict(h=None), dict(h=P + 1), dict(r=None), dict(w1=P + 2), dict(gate=P + 1), dict(q1=P + 2), dict(q2=P + 1)):
         assert fwd(B, desc(B), **kw) == -1, kw
     assert fwd(B, desc(B), ws=None) == -4 and fwd(B, desc(B), n=128) == -4 and fwd(B, desc(B), ws=P + 4) == -4
     # without a block output: no norm after it, gate or dropout; r may be left out where it is x

@@ -136,6 +136,8 @@ def test_a_block_that_is_not_finite_is_nan_and_no_other(B, bad):
     y = host(B.qbp_gemm_f8(q, s, wq, ws, transB=True))
     assert np.isnan(y[17]).all() and np.isfinite(np.delete(y, 17, 0)).all()
     assert np.array_equal(host(B.qbp_linear_f8(xt, wq, ws)), y, equal_nan=True)
+    for rows in (slice(15, 18), slice(17, 18), slice(10, 26)):                   # few rows: quantised on the way
+        assert np.array_equal(host(B.qbp_linear_f8(xt[rows], wq, ws)), y[rows], equal_nan=True)
     # a product over the rows: only the outputs of column 300
     gq, gs = B.qbp_quantize_f8(torch.from_numpy(rng(5).standard_normal((M, 32)).astype(np.float32)).cuda(), rows=False, cols=True)
     dw = host(B.qbp_gemm_f8(gq, gs, qc, sc, transA=True))
@@ -230,3 +232,29 @@ def test_linear_is_the_quantiser_and_the_product(B, M, N, K, dtype):
         assert torch.equal(B.qbp_linear_f8(x, wq, sw, w_format=fmt), want)
         assert torch.equal(B.qbp_linear_f8(x.contiguous(), wq, sw, w_format=fmt), want)
     assert B.status_word(B.workspace(256)) == 0
+
+
+def test_offsets_beyond_32_bits(B):
+    """Codes, products and quantisation of more than 2^32 elements: the last rows are those of a call on the last rows alone."""
+    import torch
+    g = torch.Generator(device="cuda"); g.manual_seed(3)
+    M, N, K, last = 70016, 65536, 256, 128
+    x = torch.randn((M, K), generator=g, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn((N, K), generator=g, device="cuda", dtype=torch.bfloat16)
+    q, s = B.qbp_quantize_f8(x)
+    wq, sw = B.qbp_quantize_f8(w)
+    y = B.qbp_gemm_f8(q, s, wq, sw, transB=True, out_dtype=torch.bfloat16)       # 4.6 G elements
+    tail = B.qbp_quantize_f8(x[-last:].contiguous())
+    assert torch.equal(q[-last:], tail[0])
+    assert torch.equal(y[-last:], B.qbp_gemm_f8(*tail, wq, sw, transB=True, out_dtype=torch.bfloat16))
+    del q, s, wq, sw, x, w
+    yq, ys, yc, ysc = B.qbp_quantize_f8(y, cols=True)
+    want = B.qbp_quantize_f8(y[-last:].contiguous(), cols=True)
+    assert torch.equal(yq[-last:], want[0]) and torch.equal(yc[-last:], want[2])
+    # a product that reads operands of that size: the last rows' outputs against 64 bits (a call on them alone adds up in another order)
+    v = torch.randn((16, N), generator=g, device="cuda", dtype=torch.bfloat16)
+    vq, vs = B.qbp_quantize_f8(v)
+    z = B.qbp_gemm_f8(vq, vs, yq, ys, transB=True)
+    a = F.values(host(vq), 0, F.spread(host(B.qbp_f8_exponents(vs, 16, N)), N))
+    b = F.values(host(want[0]), 0, F.spread(host(B.qbp_f8_exponents(want[1], last, N)), N))
+    check_on_device(z[:, -last:], a, b, N, "float32")

@@ -153,6 +153,45 @@ def test_the_norm_before_a_first_block(B, cols):
     close(dw2, (dhv * rh).sum(0), 330 * U * np.abs(dhv * rh).sum(0))
 
 
+@pytest.mark.parametrize("off", ["x", "b", "w1", "gate", "dr", "dh"])
+def test_tensors_off_the_16_byte_boundary(B, off):
+    """Any one of them: the values of the aligned call, up to the other form's order of sums."""
+    import torch
+    i = {k: v[0] for k, v in inputs(21, 512, "float32", "bfloat16", 1, 31).items()}
+    moved = torch.empty(i[off].numel() + 1, dtype=i[off].dtype, device="cuda")[1:].view(i[off].shape).copy_(i[off])
+    outs = []
+    for t in (i, {**i, off: moved}):
+        d = B.resnorm_desc(t["x"], t["b"], p=0.3, seed=4)
+        r, h, q1, q2 = B.qbp_resnorm_fwd(d, t["x"], t["b"], t["w1"], t["gate"], t["w2"])
+        outs.append((r, h, q1, q2) + B.qbp_resnorm_bwd(d, t["dr"], t["dh"], t["b"], r, q1, q2, t["w1"], t["gate"], t["w2"]))
+    # both are within the bounds above of the same values: twice the largest of them, relative to each tensor's largest value
+    for a, b in zip(*outs):
+        assert torch.equal(a == 0, b == 0) or a.dtype == torch.bfloat16
+        assert float((a.double() - b.double()).abs().max()) <= 2 * (800 * U + half_step(str(a.dtype).split(".")[1])) * 16 * float(a.double().abs().max())
+
+
+def test_more_than_2_to_the_32_elements(B):
+    """The last rows of a long join and the last elements of a long dropout are those of calls on them alone."""
+    import torch
+    rows, cols, last = 270000, 16384, 3
+    x = torch.randn(1024, cols, device="cuda", dtype=torch.bfloat16).repeat(264, 1)[:rows]
+    b = x.flip(0)
+    g = torch.rand(cols, device="cuda")
+    d = B.resnorm_desc(x, b, p=0.25, seed=6)
+    r, h, q1, q2 = B.qbp_resnorm_fwd(d, x, b, g, g, g)
+    at = (rows - last) * cols
+    e = B.resnorm_desc(x[-last:], b[-last:], p=0.25, seed=6, index_base=at)
+    r2, h2, p1, p2 = B.qbp_resnorm_fwd(e, x[-last:], b[-last:], g, g, g)
+    assert torch.equal(r[-last:], r2) and torch.equal(h[-last:], h2) and torch.equal(q1[-last:], p1)
+    dr3, dh3 = x[-last:].clone(), h2.clone()
+    dx, db, _, _, _ = B.qbp_resnorm_bwd(d, x, h, b, r, q1, q2, g, g, g, want_params=False, dx=x, db=h)
+    dx3, db3, _, _, _ = B.qbp_resnorm_bwd(e, dr3, dh3, b[-last:], r2, p1, p2, g, g, g, want_params=False)
+    assert torch.equal(dx[-last:], dx3) and torch.equal(db[-last:], db3)
+    del d, dx, db
+    y = B.qbp_dropout(r, 0.5, 9)
+    assert torch.equal(y.view(-1)[at:], B.qbp_dropout(r[-last:], 0.5, 9, index_base=at).view(-1))
+
+
 def test_outputs_over_inputs(B):
     """r over x, h over b; dx over dr, db over dh: the same bits."""
     import torch
