@@ -214,9 +214,8 @@ constexpr uint32_t kSplitSmem = 220u * 1024u;
 constexpr uint32_t kSplitCols = 256;             // tensor memory: the accumulator in [0, 128), then sets of 4 columns of scales:
 constexpr uint32_t kSplitSetU = 128, kSplitSetV = 144;
 constexpr int kSplitSets = 4, kSplitBlockSets = 16;      // of U (and of V from memory), a set for four blocks; of V quantised here, for one
-constexpr int64_t kSplitQuantise = 16;
-constexpr int kSplitDeclined = 1;                // launch_f8_split: too many rows to quantise on the way
-constexpr int kSplitAhead = 8;                   // pairs of rows that a quantising warp loads ahead
+constexpr int64_t kSplitQuantise = 16;           // rows that every CTA quantises for itself, at most
+constexpr size_t kSplitClusterSmem = 116u * 1024u;
 
 struct F8SplitParams {
     CUtensorMap mapU, mapV;                      // U: the output's columns (operand B), V: its rows (operand A)
@@ -225,7 +224,7 @@ struct F8SplitParams {
     const void *x; int64_t ld, K; int vec;       // the rows as real numbers, quantised here (no mapV, no sv)
     OperandLayout u, v;
     uint32_t idesc, stage_bytes;
-    int bn, stages, k_blocks, parts, clear;
+    int bn, stages, k_blocks, parts;
     int64_t M, N;
     void *out; int dtype;
     int *status;
@@ -278,10 +277,10 @@ template <typename T> __device__ __forceinline__ void split_add(void *out, int64
     }
 }
 
-// Warps 2..9: the blocks kb0..kb1 of all rows (at most bn) to e4m3, into the stages as the product wants them: rows of 128 bytes,
+// Warps 2..9: the blocks kb0..kb1 of all rows (at most kSplitQuantise) to e4m3, into the stages as the product wants them: rows of 128 bytes,
 // 16-byte pieces swizzled by the row, and each row's scale byte at its place in a piece.  Every eighth block is a warp's (with all warps on
 // one block, one block after the other, a block took half a microsecond, nearly all of it latency), two rows at a time, sixteen lanes to a
-// row, the next rows' loads on their way.  False when a wait ran out.
+// row, all rows' loads on their way at once.  False when a wait ran out.
 template <typename T>
 __device__ __forceinline__ bool split_quantise(const F8SplitParams &P, uint8_t *smem, uint64_t *full_bar, uint64_t *empty_bar, int kb0, int kb1)
 {
@@ -293,30 +292,27 @@ __device__ __forceinline__ bool split_quantise(const F8SplitParams &P, uint8_t *
         const int64_t c = 128ll * kb + 8 * lane16;
         const T *x = static_cast<const T *>(P.x) + (c < P.K ? c : 0);
         const auto load = [&](int r) { return load8(x + (r < M ? r : 0) * P.ld, r < M && c < P.K ? 8 : 0, P.vec != 0); };
-        Raw8<T> ahead[kSplitAhead];
+        Raw8<T> raw[kSplitQuantise / 2];
 #pragma unroll
-        for (int a = 0; a < kSplitAhead; ++a) ahead[a] = load(2 * a + high);
+        for (int a = 0; a < (int)kSplitQuantise / 2; ++a) raw[a] = load(2 * a + high);
         if (!mbar_wait_warp(&empty_bar[s / kSplitRelease], ph)) return false;
         uint8_t *const sv = smem + (size_t)s * P.stage_bytes + P.u.tile_bytes, *const bytes = sv + P.v.tile_bytes + kF8Piece + (kb & 3);
-        for (int r0 = high; r0 - high < M; r0 += 2 * kSplitAhead) {
 #pragma unroll
-            for (int a = 0; a < kSplitAhead; ++a) {
-                const int r = r0 + 2 * a;
-                if (r - high >= M) break;
-                float v[8];
-                unpack8(ahead[a], v);
-                if (r - high + 2 * kSplitAhead < M) ahead[a] = load(r + 2 * kSplitAhead);
-                float m = amax3(amax3(amax3(amax3(v[0], v[1], v[2]), v[3], v[4]), v[5], v[6]), v[7], 0.0f);
+        for (int a = 0; a < (int)kSplitQuantise / 2; ++a) {
+            const int r = 2 * a + high;
+            if (2 * a >= M) break;
+            float v[8];
+            unpack8(raw[a], v);
+            float m = amax3(amax3(amax3(amax3(v[0], v[1], v[2]), v[3], v[4]), v[5], v[6]), v[7], 0.0f);
 #pragma unroll
-                for (int o = 8; o > 0; o >>= 1) m = amax3(m, __shfl_xor_sync(0xFFFFFFFFu, m, o), 0.0f);
-                const uint32_t byte = f8_scale_byte<QBP_E4M3>(m);
-                const float inv = f8_inverse(byte);
-                if (r < M) {
+            for (int o = 8; o > 0; o >>= 1) m = amax3(m, __shfl_xor_sync(0xFFFFFFFFu, m, o), 0.0f);
+            const uint32_t byte = f8_scale_byte<QBP_E4M3>(m);
+            const float inv = f8_inverse(byte);
+            if (r < M) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], inv);
-                    *reinterpret_cast<uint2 *>(sv + r * 128 + (((lane16 >> 1) ^ (r & 7)) << 4) + (lane16 & 1) * 8) = f8_codes8<QBP_E4M3>(v);
-                    if (lane16 == 0) bytes[(r & 31) * 16 + (r >> 5) * 4] = (uint8_t)byte;
-                }
+                for (int e = 0; e < 8; ++e) v[e] = __fmul_rn(v[e], inv);
+                *reinterpret_cast<uint2 *>(sv + r * 128 + (((lane16 >> 1) ^ (r & 7)) << 4) + (lane16 & 1) * 8) = f8_codes8<QBP_E4M3>(v);
+                if (lane16 == 0) bytes[r * 16] = (uint8_t)byte;
             }
         }
         fence_proxy_async();
@@ -365,7 +361,7 @@ __global__ void __launch_bounds__(kSplitThreads, 2) f8_split_kernel(const __grid
     pdl_wait();
     // The status word is cleared here and not by a launch of its own: a wait gives up a second after it began, long after the
     // first block of a grid has started.
-    if (P.clear && threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) *P.status = 0;
+    if (threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0) *P.status = 0;
 
     if (warp == 0) {
         // (the whole warp in step, an elected lane issues, as in the pair kernel)
@@ -544,13 +540,12 @@ static int launch_f8_split(const F8Product &p, const SplitInput &in, cudaStream_
     P.stages -= P.stages % (int)kSplitRelease;
     static_assert(kSplitMaxStages + (int)kSplitRelease <= 4 * kSplitSets - 3 && kSplitMaxStages + (int)kSplitRelease < kSplitBlockSets &&
                   kSplitSetU + 4 * kSplitSets <= kSplitSetV && kSplitSetV + 4 * kSplitBlockSets <= kSplitCols, "a set of scales is written again while MMAs may read it");
-    const size_t ring = (size_t)P.stages * P.stage_bytes + sums_bytes;
+    // A cluster's CTA has an SM to itself, as the pair kernels' have: where CTAs of two clusters shared one with a third that waits for their
+    // tensor memory, while their peers wait for the third's on another SM, none would end.
+    const size_t smem = std::max<size_t>(1024 + (size_t)P.stages * P.stage_bytes + sums_bytes, P.parts > 1 ? kSplitClusterSmem : 0);
     P.M = p.M; P.N = p.N; P.out = p.out; P.dtype = p.dtype; P.status = p.status;
-    P.su = p.sB; P.groups = f8_groups(p.K); P.clear = p.cleared ? 0 : 1;
+    P.su = p.sB; P.groups = f8_groups(p.K);
     const dim3 grid((unsigned)(tiles_n * P.parts), (unsigned)tiles_m);
-    // Few rows are quantised by every CTA for itself (one call of many in a row, the quantiser apart and on the way, us: 1 x 4096 x 4096 11.5
-    // and 8.4, 16 x 1024 x 1024 8.1 and 7.1, 1 x 8192 x 8192 20.2 and 17.4; 32 x 1024 x 1024 8.3 and 9.2)
-    if (in.x && p.M > kSplitQuantise) return kSplitDeclined;
     if (in.x) {
         P.x = in.x; P.ld = in.ld; P.K = p.K;
         P.vec = aligned16(in.x) && in.ld * (int64_t)dtype_size(p.dtype) % 16 == 0 ? 1 : 0;
@@ -558,7 +553,7 @@ static int launch_f8_split(const F8Product &p, const SplitInput &in, cudaStream_
         QBP_FOR_DTYPE(p.dtype, T, {
             static PerDeviceOnce once;
             QBP_SMEM_OPT_IN(once, f8_split_kernel<T>, kSplitSmem);
-            launch_clusters(f8_split_kernel<T>, grid, (unsigned)P.parts, kSplitThreads, 1024 + ring, st, P);
+            launch_clusters(f8_split_kernel<T>, grid, (unsigned)P.parts, kSplitThreads, smem, st, P);
         });
         QBP_LAUNCH_OK("f8_split_kernel<quantise>");
         return QBP_OK;
@@ -566,7 +561,7 @@ static int launch_f8_split(const F8Product &p, const SplitInput &in, cudaStream_
     P.sv = p.sA;
     if ((rc = p.transA ? make_map_2d(&P.mapV, p.A, p.K, p.M, 128, 128) : make_map_2d(&P.mapV, p.A, p.M, p.K, (uint32_t)P.bn, 128))) return rc;
     QBP_TRACE_BEGIN(st);
-    launch_clusters(f8_split_kernel<FromCodes>, grid, (unsigned)P.parts, kSplitThreads, 1024 + ring, st, P);
+    launch_clusters(f8_split_kernel<FromCodes>, grid, (unsigned)P.parts, kSplitThreads, smem, st, P);
     QBP_LAUNCH_OK("f8_split_kernel");
     return QBP_OK;
 }
@@ -649,7 +644,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_gemm_f8(int transA, in
                                                                   void *out, void *ws, size_t ws_bytes, void *stream)
 {
     cudaStream_t st = (cudaStream_t)stream;
-    F8Product p{transA, transB, M, N, K, formatA, formatB, A, sA, B, sB, out, out_dtype, static_cast<int *>(ws), false};
+    F8Product p{transA, transB, M, N, K, formatA, formatB, A, sA, B, sB, out, out_dtype, static_cast<int *>(ws)};
     int rc = check_product(p, "gemm_f8");
     if (rc) return rc;
     if (!ws || !aligned_to(ws, 256) || ws_bytes < qbp_gemm_f8_workspace_bytes(M, N, K))
@@ -677,7 +672,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_linear_f8(const void *
                                                                     const uint8_t *w, const uint8_t *sw, void *y, void *ws, size_t ws_bytes, void *stream)
 {
     cudaStream_t st = (cudaStream_t)stream;
-    F8Product p{0, 1, M, N, K, QBP_E4M3, w_format, nullptr, nullptr, w, sw, y, dtype, static_cast<int *>(ws), false};
+    F8Product p{0, 1, M, N, K, QBP_E4M3, w_format, nullptr, nullptr, w, sw, y, dtype, static_cast<int *>(ws)};
     int rc = check_product(p, "linear_f8");
     if (rc) return rc;
     if ((rc = check_quantize("linear_f8", x, dtype, M, K, ld, QBP_E4M3))) return rc;
@@ -691,7 +686,9 @@ extern "C" __attribute__((visibility("default"))) int qbp_linear_f8(const void *
         return QBP_OK;
     }
     if (!w || !sw || !aligned16(w) || !aligned16(sw)) return fail(QBP_ERR_INVALID_ARG, "linear_f8: the weights or their scales are NULL or not on a 16-byte boundary");
-    if (one_wave(p) && (rc = launch_f8_split(p, SplitInput{x, ld}, st)) != kSplitDeclined) return rc;
+    // Few rows are quantised by every CTA for itself (one call of many in a row, the quantiser apart and on the way, us: 1 x 4096 x 4096 11.5
+    // and 8.4, 16 x 1024 x 1024 8.1 and 7.1, 1 x 8192 x 8192 20.2 and 17.4; 32 x 1024 x 1024 8.3 and 9.2)
+    if (M <= kSplitQuantise) return launch_f8_split(p, SplitInput{x, ld}, st);
     WsCarver c(ws, ws_bytes);
     c.take<int>(1);
     uint8_t *q = c.take<uint8_t>((size_t)M * (size_t)K), *s = c.take<uint8_t>(qbp_f8_scale_bytes(M, K));

@@ -37,7 +37,7 @@ struct F8Product {
     int formatA, formatB;
     const uint8_t *A, *sA, *B, *sB;
     void *out; int dtype;
-    int *status; bool cleared;                                    // whether the status word is zero already
+    int *status;
 };
 int launch_f8_pair(const F8Product &p, cudaStream_t st);
 

@@ -48,7 +48,7 @@ struct F8PairParams {
     int tiles_m, tiles_n, tiles_total, pairs;
     FastDiv d_group;
     int64_t M, N;
-    void *out; int dtype, tma_out, clear;
+    void *out; int dtype, tma_out;
     int *status;
 };
 
@@ -175,7 +175,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFpThreads, 1) f8_pa
     bool timed_out = false;
     pdl_wait();
     // (cleared here and not by a launch of its own: a wait gives up a second after it began, long after a grid's first block has started)
-    if (P.clear && blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;
 
     if (warp == 0) {
         // (the whole warp in step, an elected lane issues: addresses and coordinates then stay in uniform registers, where the copies
@@ -346,7 +346,7 @@ int launch_f8_pair(const F8Product &p, cudaStream_t st)
     P.stages = std::min<int>(kFpMaxStages, (int)((kFpSmem - 1024 - kFpEpiWarps * kFpSlab) / P.stage_bytes));
     P.stages -= P.stages % (int)kFpRelease;                          // 6 or 8
     static_assert(kFpMaxStages + kFpRelease <= 17, "a set of scales is written again while MMAs may read it");
-    P.M = p.M; P.N = p.N; P.out = p.out; P.dtype = p.dtype; P.status = p.status; P.clear = p.cleared ? 0 : 1;
+    P.M = p.M; P.N = p.N; P.out = p.out; P.dtype = p.dtype; P.status = p.status;
     const size_t smem = 1024 + (size_t)P.stages * P.stage_bytes + kFpEpiWarps * kFpSlab;
     static PerDeviceOnce configured;
     QBP_SMEM_OPT_IN(configured, f8_pair_kernel, kFpSmem);

@@ -52,33 +52,6 @@ template <typename T> __device__ __forceinline__ Raw8<T> pack8(const float (&v)[
     return r;
 }
 
-// Two fp32 values that one instruction works on.
-struct Pair { unsigned long long u; };
-__device__ __forceinline__ Pair pair_of(float a, float b)
-{
-    Pair p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p.u) : "f"(a), "f"(b));
-    return p;
-}
-__device__ __forceinline__ Pair pair_of(float a) { return pair_of(a, a); }
-__device__ __forceinline__ void split(Pair p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.u)); }
-__device__ __forceinline__ float sum_of(Pair p) { float a, b; split(p, a, b); return a + b; }
-__device__ __forceinline__ Pair pair_mul(Pair a, Pair b) { Pair r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u)); return r; }
-__device__ __forceinline__ Pair pair_fma(Pair a, Pair b, Pair c) { Pair r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u)); return r; }
-template <typename T> __device__ __forceinline__ void unpack_pairs(const Raw8<T> &r, Pair (&v)[4])
-{
-    float f[8];
-    unpack8(r, f);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = pair_of(f[2 * i], f[2 * i + 1]);
-}
-template <typename T> __device__ __forceinline__ Raw8<T> pack_pairs(const Pair (&v)[4])
-{
-    float f[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) split(v[i], f[2 * i], f[2 * i + 1]);
-    return pack8<T>(f);
-}
 // The first `n` (at most 8) of eight elements at p, zeros behind them; vec: p is on a 16-byte boundary.
 template <typename T> __device__ __forceinline__ Raw8<T> load8(const T *p, int n, bool vec)
 {

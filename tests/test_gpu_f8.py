@@ -234,6 +234,50 @@ def test_linear_is_the_quantiser_and_the_product(B, M, N, K, dtype):
     assert B.status_word(B.workspace(256)) == 0
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_of_rows_off_the_16_byte_boundary(B, dtype):
+    import torch
+    w = torch.from_numpy(rng(1).standard_normal((200, 400)).astype(np.float32)).cuda()
+    wq, sw, _ = B.qbp_quantize_f8_square(w)
+    for M in (1, 2, 9, 16, 17, 50):
+        x = torch.from_numpy(wide_values(M, 407, M).astype(np.float32)).to(getattr(torch, dtype)).cuda()[:, 3:403]
+        assert torch.equal(B.qbp_linear_f8(x, wq, sw), B.qbp_linear_f8(x.contiguous(), wq, sw))
+
+
+@pytest.mark.parametrize("M,N,K,transA,transB", [(5, 256, 640, False, True), (100, 272, 1024, False, False), (144, 300, 512, True, True), (2600, 2112, 640, False, True),
+                                                 (2608, 2112, 640, True, False)])
+def test_a_nan_enters_its_own_outputs_alone(B, M, N, K, transA, transB):
+    import torch
+    x = torch.from_numpy(wide_values(M, K, 1).astype(np.float32)).cuda()
+    y = torch.from_numpy(wide_values(N, K, 2).astype(np.float32)).cuda()
+    ops = lambda x, y: B.qbp_quantize_f8(x.t().contiguous() if transA else x, rows=not transA, cols=transA) + B.qbp_quantize_f8(y if transB else y.t().contiguous(), rows=transB, cols=not transB)
+    good = B.qbp_gemm_f8(*ops(x, y), transA=transA, transB=transB)
+    assert bool(torch.isfinite(good).all())
+    x[M // 2, K - 1] = float("nan"); y[3, 0] = float("inf")
+    got = B.qbp_gemm_f8(*ops(x, y), transA=transA, transB=transB)
+    bad = torch.zeros((M, N), dtype=torch.bool, device="cuda")
+    bad[M // 2] = True; bad[:, 3] = True
+    assert torch.equal(torch.isnan(got), bad) and torch.equal(got[~bad], good[~bad])
+
+
+def test_small_products_of_many_streams(B):
+    """Products in clusters that come to the SMs together: each has the tensor memory it needs, and the results are those of one at a time."""
+    import torch
+    shapes = [(1, 1024, 2048), (16, 512, 4096), (3, 2048, 1536), (40, 768, 2048), (100, 512, 2048), (128, 1024, 1024)]
+    cases = []
+    for i, (M, N, K) in enumerate(shapes):
+        x = torch.from_numpy(wide_values(M, K, i).astype(np.float32)).cuda()
+        wq, sw, _ = B.qbp_quantize_f8_square(torch.from_numpy(rng(i).standard_normal((N, K)).astype(np.float32)).cuda())
+        cases.append((x, wq, sw, B.qbp_linear_f8(x, wq, sw), torch.cuda.Stream(), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    outs = [[torch.empty_like(c[3]) for _ in range(20)] for c in cases]
+    for k in range(20):
+        for (x, wq, sw, _, stream, ws), o in zip(cases, outs):
+            with torch.cuda.stream(stream): B.qbp_linear_f8(x, wq, sw, y=o[k], ws=ws)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, c[3]) for c, o in zip(cases, outs) for y in o) and all(B.status_word(c[5]) == 0 for c in cases)
+
+
 def test_offsets_beyond_32_bits(B):
     """Codes, products and quantisation of more than 2^32 elements: the last rows are those of a call on the last rows alone."""
     import torch
