@@ -660,7 +660,7 @@ int qbp_quantize_f8_square(const void *x, int dtype, int64_t rows, int64_t cols,
  * outer = M, sB over outer = N, both over reduction = K.  An operand's innermost stored
  * extent is a multiple of 16, the other extents are free; M or N of zero: nothing is done;
  * K of zero: out is cleared.  The device status word is the start of `ws`, as
- * for qbp_gemm_s8. */
+ * for qbp_gemm_s8 (of qbp_linear_f8 as well). */
 size_t qbp_gemm_f8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 
 int qbp_gemm_f8(int transA, int transB, int64_t M, int64_t N, int64_t K,
@@ -696,7 +696,8 @@ int qbp_linear_f8(const void *x, int dtype, int64_t ld, int64_t M, int64_t N, in
  * x and r have x_dtype, b and h b_dtype; rows of any number, cols up to
  * QBP_RESNORM_MAX_COLS, every tensor aligned to its element (16 bytes and cols a multiple of 8:
  * faster).  rstd_post / rstd_pre [rows] (nullable) receive 1 / RMS for the backward pass.
- * r may be x, and h may be b.  ws: 256 bytes, whose first four are the device status word (see
+ * r may be x, and h may be b.  Squares are summed in fp32: a row whose sum of squares passes 3.4e38 has
+ * a norm of zeros.  ws: 256 bytes, whose first four are the device status word (see
  * Conventions), of the backward pass as well.
  * ---------------------------------------------------------------------- */
 #define QBP_RESNORM_MAX_COLS 16384
@@ -735,7 +736,8 @@ int qbp_resnorm_bwd(const qbp_resnorm_desc *d, const void *dr, const void *dh, c
  * never stored: the backward pass is the same call on the gradient.  Draws are 16 bits of a
  * Philox4x32-10 word, eight to a block: key = seed, counter = (i/8 low, i/8 high, tensor_id,
  * 0xFFFFFFFF), word (i / 2) % 4, its low half for even i (the stochastic quantisers'
- * counters end in other words: equal ids do not correlate).  n elements of the type, any
+ * counters end in other words: equal ids do not correlate).  Seed, id and index are arguments of
+ * the call: a captured one repeats its draws at each replay.  n elements of the type, any
  * alignment of their type; y may be x; index_base a multiple of 8. */
 int qbp_dropout(const void *x, int dtype, int64_t n, float p, uint64_t seed, uint32_t tensor_id, uint64_t index_base,
                 void *y, void *stream);

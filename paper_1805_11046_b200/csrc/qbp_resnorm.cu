@@ -1,7 +1,7 @@
 // The join between two blocks of a residual network and its gradients (qbp_resnorm_fwd / _bwd in include/qbp.h): norm after a
 // block, gate, dropout, residual stream and the norm before the next block, in one pass over the rows.
 //
-// A row is held in registers by the threads of one group: a warp (of a block's eight) for rows of up to 256 columns, a block of
+// A row is held in registers by the threads of one group: a warp (of a block's eight) for rows of up to 512 columns, a block of
 // up to 512 threads beyond; a thread has CH times eight columns.  The two sums over a row (of b^2 and of r^2; backwards of the
 // gradients' projections on r and b) are exchanged between the group's threads, forward a row's second with the next row's first, backwards
 // both at once, and nothing is read twice.  A block
@@ -196,8 +196,8 @@ template <bool WARP> __device__ __forceinline__ void end_row(int pre, int post)
 // ---- rows read in vectors, through the ring ------------------------------------------------------------------------------
 // A row is copied by a lane of its group's first warp, whose bytes a slot's barrier reports (full).  Forward a slot is free for the next
 // copy once its row's sums have been exchanged; backwards, where a row is read behind the exchange too, each warp says so (empty).  Every wait
-// is bounded: a warp whose wait ran out raises the status word, waits for nothing any more and goes through the rest of its rows for
-// the block's barriers' sake.
+// is bounded: a warp whose wait ran out raises the status word, gives copies in flight another millisecond, copies and waits for nothing any
+// more and goes through the rest of its rows for the block's barriers' sake.
 template <typename T> struct Pieces { static constexpr int n = sizeof(T) / 2; };
 constexpr int kJoinSlots = 3, kJoinBackSlots = 2;
 struct JoinBars { uint64_t full[kJoinWarpRows][kJoinSlots], empty[kJoinBackSlots]; };
@@ -233,7 +233,7 @@ struct JoinPlace {
 };
 __device__ __forceinline__ void join_wait(uint64_t *bar, uint32_t parity, bool &dead, int *status)
 {
-    if (!dead && !mbar_wait_uniform(bar, parity)) { dead = true; raise_timeout(status); }
+    if (!dead && !mbar_wait_uniform(bar, parity)) { dead = true; raise_timeout(status); __nanosleep(1000000); }
 }
 // Eight columns of a row in a slot (zero behind the last one).
 template <typename T> __device__ __forceinline__ void ring_read(const uint8_t *row, int c, bool in, float (&v)[8])
@@ -286,8 +286,9 @@ join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ Ph
     uint8_t *const slots = ring + (uint32_t)(sub * kJoinSlots) * slot_bytes;
     uint64_t *const full = bars.full[sub];
     const JoinSource src[2] = {{P.x, row_x, 0u}, {P.b, row_b, row_x}};
+    bool dead = false;
     const auto fetch = [&](int64_t row, int64_t end, uint32_t slot) {
-        if ((WARP || warp == 0) && row < end) join_copy<2>(slots + slot * slot_bytes, &full[slot], src, row);
+        if ((WARP || warp == 0) && row < end && !dead) join_copy<2>(slots + slot * slot_bytes, &full[slot], src, row);
     };
     bool in[CH];
     float gw[CH][8], w2[CH][8];
@@ -311,7 +312,6 @@ join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ Ph
     int64_t had = -1;
     int half = 0;
     JoinPlace place{0u, 0u};
-    bool dead = false;
     for (int64_t item = blockIdx.x; item < P.it.gates * P.it.splits; item += gridDim.x) {
         const ItemRows rows = item_rows(P.it, item);
         if (P.b && rows.gate != had) {
@@ -878,6 +878,12 @@ static int check_join(const qbp_resnorm_desc *d, const char *name, const void *b
         if (!aligned_to(w, 4)) return fail(QBP_ERR_INVALID_ARG, "%s: misaligned parameters", name);
     return QBP_OK;
 }
+// A call with nothing to do (a workspace that is there gets its status word cleared all the same).
+static int join_empty(void *ws, size_t ws_bytes, cudaStream_t st)
+{
+    if (ws && aligned_to(ws, 4) && ws_bytes >= 4) QBP_CUDA_OK(cudaMemsetAsync(ws, 0, 4, st));
+    return QBP_OK;
+}
 static bool real_ok(const void *p, int dtype) { return p && aligned_to(p, dtype_size(dtype)); }
 static int64_t join_gates(const qbp_resnorm_desc *d) { return d->gate_rows ? (d->rows + d->gate_rows - 1) / d->gate_rows : 1; }
 
@@ -897,6 +903,8 @@ static JoinCut join_cut(const qbp_resnorm_desc *d, const JoinShape &s, bool per_
     c.blocks = std::min(most, it.gates * it.splits);
     return c;
 }
+// Partial rows of dgate: none where an item is all of a gate's rows, whose sum is the gradient.
+static size_t gate_parts(const JoinItems &it) { return it.splits > 1 ? (size_t)(it.gates * it.splits * it.cols) : 0; }
 // Blocks of a wave: 16 warps an SM (8 backwards where a row is a warp's), which their registers allow, or what their rings leave room for.
 static int64_t join_blocks(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
 {
@@ -916,7 +924,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_fwd(const qbp_
     cudaStream_t st = (cudaStream_t)stream;
     int rc = check_join(d, "resnorm_fwd", b, gate, w_post, w_pre);
     if (rc) return rc;
-    if (d->rows == 0 || d->cols == 0) return QBP_OK;
+    if (d->rows == 0 || d->cols == 0) return join_empty(ws, ws_bytes, st);
     if (!real_ok(x, d->x_dtype) || (b && !real_ok(b, d->b_dtype)) || (r && !real_ok(r, d->x_dtype)) || (d->pre && !real_ok(h, d->b_dtype)))
         return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: a tensor is NULL or misaligned");
     if (!aligned_to(rstd_post, 4) || !aligned_to(rstd_pre, 4)) return fail(QBP_ERR_INVALID_ARG, "resnorm_fwd: misaligned fp32 tensors");
@@ -958,7 +966,7 @@ extern "C" __attribute__((visibility("default"))) size_t qbp_resnorm_bwd_workspa
     size_t most = 0;
     for (bool per_gate : {false, true}) {
         const JoinCut c = join_cut_bwd(d, per_gate);
-        most = std::max(most, 2 * align_up((size_t)(c.blocks * d->cols) * 4, 256) + align_up((size_t)(c.it.gates * c.it.splits * d->cols) * 4, 256));
+        most = std::max(most, 2 * align_up((size_t)(c.blocks * d->cols) * 4, 256) + align_up(gate_parts(c.it) * 4, 256));
     }
     return 256 + most;
 }
@@ -974,12 +982,12 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
     for (const float *w : {(const float *)dw_post, (const float *)dgate, (const float *)dw_pre, rstd_post, rstd_pre})
         if (!aligned_to(w, 4)) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: misaligned fp32 tensors");
     if ((dw_post && !d->post) || (dw_pre && !d->pre)) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: gradients of a norm that is not there");
-    if (d->cols == 0) return QBP_OK;
+    if (d->cols == 0) return join_empty(ws, ws_bytes, st);
     if (d->rows == 0) {                              // (no gates but for one that all rows share)
         if (dw_post) QBP_CUDA_OK(cudaMemsetAsync(dw_post, 0, (size_t)d->cols * 4, st));
         if (dw_pre) QBP_CUDA_OK(cudaMemsetAsync(dw_pre, 0, (size_t)d->cols * 4, st));
         if (dgate && !d->gate_rows) QBP_CUDA_OK(cudaMemsetAsync(dgate, 0, (size_t)d->cols * 4, st));
-        return QBP_OK;
+        return join_empty(ws, ws_bytes, st);
     }
     if ((db || dgate) && !b) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: gradients of a block output that is NULL");
     if (!dx && !db && !dw_post && !dgate && !dw_pre) return fail(QBP_ERR_INVALID_ARG, "resnorm_bwd: no output wanted");
@@ -990,7 +998,6 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
     if (!ws || !aligned_to(ws, 256) || ws_bytes < qbp_resnorm_bwd_workspace_bytes(d))
         return fail(QBP_ERR_WORKSPACE, "resnorm_bwd: workspace NULL, misaligned or smaller than %zu bytes", qbp_resnorm_bwd_workspace_bytes(d));
     const JoinCut c = join_cut_bwd(d, gate || dgate);
-    const int64_t items = c.it.gates * c.it.splits;
     WsCarver w(ws, ws_bytes);
     JoinBwdParams P{};
     P.status = w.take<int>(1);
@@ -999,9 +1006,8 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
     P.dx = dx; P.db = db; P.alpha = d->alpha; P.inv_cols = (float)(1.0 / (double)d->cols);
     P.post = d->post ? 1 : 0; P.pre = d->pre ? 1 : 0; P.x_dtype = d->x_dtype; P.b_dtype = d->b_dtype;
     P.part_post = w.take<float>((size_t)(c.blocks * d->cols)); P.part_pre = w.take<float>((size_t)(c.blocks * d->cols));
-    P.part_gate = w.take<float>((size_t)(items * d->cols));
     P.sum_post = dw_post ? 1 : 0; P.sum_pre = dw_pre ? 1 : 0; P.sum_gate = dgate ? 1 : 0;
-    if (dgate && c.it.splits == 1) P.part_gate = dgate;
+    P.part_gate = c.it.splits > 1 ? w.take<float>(gate_parts(c.it)) : dgate;
     if (dw_post && c.blocks == 1) P.part_post = dw_post;
     if (dw_pre && c.blocks == 1) P.part_pre = dw_pre;
     P.d = dropout_params(d->p, d->tensor_id, d->index_base);

@@ -95,14 +95,35 @@ def test_joins(B):
     assert bwd(B, desc(B), b=None) == -1                                # db of no block output
     assert bwd(B, desc(B, post=0)) == -1 and bwd(B, desc(B, pre=0)) == -1          # gradients of norms that are not there
     assert bwd(B, desc(B, pre=0), dr=None, dw2=None) == -1              # neither r nor h has a gradient
-    assert bwd(B, desc(B), ws=None) == -4 and bwd(B, desc(B), n=1000) == -4 and bwd(B, desc(B), ws=P + 16) == -4
-    assert fwd(B, desc(B, rows=0)) == 0 and fwd(B, desc(B, cols=0)) == 0 and bwd(B, desc(B, cols=0)) == 0
+    assert bwd(B, desc(B), ws=None) == -4 and bwd(B, desc(B), n=700) == -4 and bwd(B, desc(B), ws=P + 16) == -4
+    assert all(f(B, desc(B, **kw), ws=None) == 0 for f, kw in ((fwd, dict(rows=0)), (fwd, dict(cols=0)), (bwd, dict(cols=0))))
 
 
 def test_join_workspace_covers_every_cut(B):
+    need = lambda **kw: B.qbp_resnorm_bwd_workspace_bytes(desc(B, **kw))
     for kw in (dict(rows=1), dict(rows=10 ** 6), dict(cols=1), dict(cols=16384, rows=9), dict(rows=1000, gate_rows=1), dict(rows=1000, gate_rows=999), dict(rows=0)):
-        assert B.lib.qbp_resnorm_bwd_workspace_bytes(C.addressof(desc(B, **kw))) >= 256
-    assert B.lib.qbp_resnorm_bwd_workspace_bytes(C.addressof(desc(B, rows=1000, gate_rows=1))) >= 1000 * 64 * 4
+        assert need(**kw) >= 256
+    # a partial row of each gate's gradient for each of its items, but none where a gate's rows are one item
+    few, many = need(rows=10 ** 6, gate_rows=1), need(rows=10 ** 6, gate_rows=10 ** 6)
+    assert few <= many and few < 10 ** 6 * 64 * 4 and many >= 3 * 100 * 64 * 4
+
+
+def test_a_layers_words_and_scratch():
+    """Each call has a status word of its own; outgrown workspaces stay where they are."""
+    import torch
+    from paper_1805_11046_b200 import layer
+    s = layer._F8Space(3, "cpu")
+    assert s.status() == 0
+    a = s.at(1)
+    a[:4].view(torch.int32)[0] = -6
+    assert s.status() == -6 and s.get().numel() == 768 and s.at(2).data_ptr() == a.data_ptr() + 256
+    b = s.at(2, 5000)
+    assert b.numel() >= 5256 and b.data_ptr() % 256 == s.get().data_ptr() % 256 and s.at(1).data_ptr() != a.data_ptr()
+    assert s.status() == -6 and int(a[:4].view(torch.int32)[0]) == -6
+    a[:4] = 0
+    assert s.status() == 0
+    for n in range(5000, 9000, 7): s.get(n)
+    assert len(s.kept) <= 4 and sum(t.numel() for t in s.kept) <= 2 * s.get().numel()
 
 
 def test_dropout(B):
