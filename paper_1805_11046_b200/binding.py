@@ -546,14 +546,17 @@ def qbp_quantize_f8(x, format=QBP_E4M3, rows=True, cols=False):
     return (qr, sr, qc, sc) if rows and cols else (qr, sr) if rows else (qc, sc)
 
 
-def qbp_quantize_f8_square(x, format=QBP_E4M3):
+def qbp_quantize_f8_square(x, format=QBP_E4M3, out=None):
     """Codes of x [rows, columns] with one scale for each 128 x 128 block, and the scales for products that reduce over the
-    columns and over the rows: (q, s_rows, s_cols)."""
-    device = _here(x)
+    columns and over the rows: (q, s_rows, s_cols).  out: an earlier call's three tensors, to be written again."""
+    device = _here(x, *(out or ()))
     r, c, ld = _rows_of(x)
-    q, sr, sc = _new(x.shape, torch.uint8, device), _new(_scale_bytes(r, c), torch.uint8, device), _new(_scale_bytes(c, r), torch.uint8, device)
-    _check(lib.qbp_quantize_f8_square(x.data_ptr(), _dtype(x.dtype), r, c, ld, format, q.data_ptr(), sr.data_ptr(), sc.data_ptr(),
-                                      _stream_handle(device)))
+    if out is None:
+        out = _new(x.shape, torch.uint8, device), _new(_scale_bytes(r, c), torch.uint8, device), _new(_scale_bytes(c, r), torch.uint8, device)
+    elif out[0].shape != x.shape: raise ValueError(f"out is {tuple(out[0].shape)}, x {tuple(x.shape)}")
+    else: _scales_fit(out[1], r, c, "s_rows"); _scales_fit(out[2], c, r, "s_cols")
+    q, sr, sc = out
+    _check(lib.qbp_quantize_f8_square(x.data_ptr(), _dtype(x.dtype), r, c, ld, format, _codes(q), _codes(sr), _codes(sc), _stream_handle(device)))
     return q, sr, sc
 
 

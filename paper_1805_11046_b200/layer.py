@@ -185,52 +185,79 @@ class TernarizedLayer:
         return dx, dw, dgamma, dbeta
 
 
+class _F8Space:
+    """A layer's own workspaces: `words` of 256 bytes, each a call's status word (cleared), and the calls' scratch behind them.
+    Outgrown ones are kept, because a captured graph keeps the addresses of its calls (each is twice the last one at least, so that they
+    add up to no more than the newest)."""
+
+    def __init__(self, words, device):
+        self.words, self.device, self.kept = words, device, []
+
+    def get(self, scratch=0):
+        """The workspace, with at least so many bytes behind its words."""
+        need = 256 * self.words + scratch
+        if not self.kept or self.kept[-1].numel() < need:
+            size = max(need, 2 * self.kept[-1].numel() if self.kept else 0)
+            self.kept.append(torch.zeros(-(-size // 256) * 256, dtype=torch.uint8, device=self.device))
+        return self.kept[-1]
+
+    def at(self, word, scratch=0):
+        """For a call that takes its status word and scratch in one piece: the workspace from a word on.  The call's scratch lies
+        over the words behind it, whose calls have to follow this one."""
+        return self.get(scratch)[256 * word:]
+
+    def status(self) -> int:
+        """0, or the status of a call that failed (synchronises the current stream)."""
+        return min(int(t[:256 * self.words].view(torch.int32)[::64].min()) for t in self.kept) if self.kept else 0
+
+
 class F8Linear:
     """A linear layer y = x w^T in 8-bit floating point with a scale for each block of 128: the activation and the gradient are
     quantised along their rows for y and dx and along their columns for dw, the fp32 master weights w [out_features,
     in_features] in 128 x 128 blocks, once per forward.  Call order and buffers only.  grad_format: B.QBP_E5M2 gives the gradient
-    the wider range."""
+    the wider range.  A layer's calls follow one another (its workspace, codes and saved tensors are its own); in a captured graph
+    they keep their addresses: the codes are written again in place, so that a captured serve() answers with the weights as the last
+    quantise() or forward() found them."""
 
     def __init__(self, w, grad_format=B.QBP_E4M3):
         self.w, self.grad_format = w, grad_format
-        self.ws = torch.empty(256, dtype=torch.uint8, device=w.device)          # of its own: a captured step keeps its address
+        self.space = _F8Space(4, w.device)                                      # dw, dx, y, serve
         self.codes = self.saved = self.dw = None
 
     def quantise(self):
         """The weights' codes and scales, as a layer that serves keeps them until its weights change."""
-        self.codes = B.qbp_quantize_f8_square(self.w)
+        self.codes = B.qbp_quantize_f8_square(self.w, out=self.codes)
         return self.codes
 
     def serve(self, x):
-        """y for an activation of any number of rows, from the codes quantise() left."""
-        q, s, _ = self.codes
-        need = B.qbp_linear_f8_workspace_bytes(x.numel() // max(x.shape[-1], 1), *q.shape)
-        if self.ws.numel() < need: self.ws = torch.empty(need, dtype=torch.uint8, device=x.device)
-        return B.qbp_linear_f8(x, q, s, ws=self.ws)
+        """y for an activation of any number of rows, from the codes that quantise() or forward() left."""
+        q, s, _ = self.codes or self.quantise()
+        return B.qbp_linear_f8(x, q, s, ws=self.space.at(3, B.qbp_linear_f8_workspace_bytes(x.numel() // max(x.shape[-1], 1), *q.shape)))
 
     def forward(self, x):
         q, s, _ = self.quantise()
         xq, sx, xqt, sxt = B.qbp_quantize_f8(x, cols=True)
         self.saved = (xqt, sxt)
-        return B.qbp_gemm_f8(xq, sx, q, s, transB=True, out_dtype=x.dtype, ws=self.ws)
+        return B.qbp_gemm_f8(xq, sx, q, s, transB=True, out_dtype=x.dtype, ws=self.space.at(2))
 
     def backward(self, g):
         """dx in g's type; the weights' gradient is left in dw (fp32)."""
         q, _, st = self.codes
         xqt, sxt = self.saved
         gq, sg, gqt, sgt = B.qbp_quantize_f8(g, format=self.grad_format, cols=True)
-        dx = B.qbp_gemm_f8(gq, sg, q, st, formatA=self.grad_format, out_dtype=g.dtype, ws=self.ws)
-        self.dw = B.qbp_gemm_f8(gqt, sgt, xqt, sxt, transA=True, formatA=self.grad_format, out=self.dw, ws=self.ws)
+        dx = B.qbp_gemm_f8(gq, sg, q, st, formatA=self.grad_format, out_dtype=g.dtype, ws=self.space.at(1))
+        self.dw = B.qbp_gemm_f8(gqt, sgt, xqt, sxt, transA=True, formatA=self.grad_format, out=self.dw, ws=self.space.at(0))
         return dx
 
     def status(self) -> int:
-        return B.status_word(self.ws)
+        return self.space.status()
 
 
 class F8ResidualStack:
     """Residual blocks of one linear layer each: h = norm(x) w_pre, and for every block b = linear(h), r = alpha x + gate *
     dropout(norm(b) w_post), the next block's h = norm(r) w_pre, with the join after a block and before the next one as one pass.
-    Master weights, norms and gates are fp32 and updated by qbp_sgd_update_many.  Call order and buffers only."""
+    Master weights, norms and gates are fp32 and updated by qbp_sgd_update_many.  Call order and buffers only.  A captured step
+    repeats its draws of the dropout: their number is an argument of its calls."""
 
     def __init__(self, weights, alpha=1.0, eps=1e-6, p=0.0, seed=0, lr=0.1, momentum=0.9, weight_decay=0.0, grad_format=B.QBP_E5M2):
         """weights: [C, C] fp32 device tensors, one for each block, updated in place."""
@@ -243,21 +270,19 @@ class F8ResidualStack:
         self.step = 0
         self.velocity = None
         self.saved = self.grads = None
-        self.ws = torch.empty(256, dtype=torch.uint8, device=dev)               # of the joins
+        self.space = _F8Space(2 * (len(weights) + 1), dev)                      # the joins forward, then backward in their order
 
     def forward(self, x, h_dtype=torch.bfloat16):
         """x [rows, C]: the residual stream, of its own type.  Returns the last block's h (h_dtype)."""
         n = len(self.linears)
         first = B.resnorm_desc(x, eps=self.eps, h_dtype=h_dtype)
-        need = B.qbp_resnorm_bwd_workspace_bytes(first)
-        if self.ws.numel() < need: self.ws = torch.empty(need, dtype=torch.uint8, device=x.device)
-        _, h, _, q = B.qbp_resnorm_fwd(first, x, w_pre=self.w_first, ws=self.ws)
+        _, h, _, q = B.qbp_resnorm_fwd(first, x, w_pre=self.w_first, ws=self.space.at(0))
         joins, r = [], x
         for i, lin in enumerate(self.linears):
             b = lin.forward(h)
             # (a stream of draws for each block and step)
             d = B.resnorm_desc(r, b, alpha=self.alpha, eps=self.eps, p=self.p, seed=self.seed, tensor_id=self.step * n + i)
-            r, h, q1, q2 = B.qbp_resnorm_fwd(d, r, b, self.w_post[i], self.gate[i], self.w_pre[i], ws=self.ws)
+            r, h, q1, q2 = B.qbp_resnorm_fwd(d, r, b, self.w_post[i], self.gate[i], self.w_pre[i], ws=self.space.at(1 + i))
             joins.append((d, b, r, q1, q2))
         self.saved = (first, x, q, joins)
         return h
@@ -266,12 +291,13 @@ class F8ResidualStack:
         """dh: the gradient at forward's result.  Returns the gradient at x; the parameters' are left in grads."""
         first, x, q, joins = self.saved
         dr, grads = None, []
+        n, need = len(joins), B.qbp_resnorm_bwd_workspace_bytes(first)
         for i in reversed(range(len(joins))):
             d, b, r, q1, q2 = joins[i]
-            dr, db, dw1, dg, dw2 = B.qbp_resnorm_bwd(d, dr, dh, b, r, q1, q2, self.w_post[i], self.gate[i], self.w_pre[i], ws=self.ws)
+            dr, db, dw1, dg, dw2 = B.qbp_resnorm_bwd(d, dr, dh, b, r, q1, q2, self.w_post[i], self.gate[i], self.w_pre[i], ws=self.space.at(2 * n - i, need))
             dh = self.linears[i].backward(db)
             grads.append((self.linears[i].dw, dw1, dg.view(-1), dw2))
-        dx, _, _, _, dw = B.qbp_resnorm_bwd(first, dr, dh, None, x, None, q, w_pre=self.w_first, ws=self.ws)
+        dx, _, _, _, dw = B.qbp_resnorm_bwd(first, dr, dh, None, x, None, q, w_pre=self.w_first, ws=self.space.at(2 * n + 1, need))
         self.grads = (grads[::-1], dw)
         return dx
 
@@ -285,4 +311,4 @@ class F8ResidualStack:
         self.step += 1
 
     def status(self) -> int:
-        return min([B.status_word(self.ws)] + [lin.status() for lin in self.linears])
+        return min([self.space.status()] + [lin.status() for lin in self.linears])

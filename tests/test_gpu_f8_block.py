@@ -196,6 +196,52 @@ def test_serving_from_kept_codes(B):
     assert L.serve(x[:0]).shape == (0, 400)
 
 
+def test_a_captured_serve_outlives_larger_calls_and_new_weights(B):
+    """A graph of serve() keeps its workspace when a later call needs a larger one, and answers with the weights as quantised last."""
+    import torch
+    from paper_1805_11046_b200 import layer
+    w = torch.from_numpy(rng(18).standard_normal((256, 384)).astype(np.float32) * 0.05).cuda()
+    x = real(rng(19).standard_normal((40, 384)), "bfloat16")[0]
+    L = layer.F8Linear(w)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side): L.serve(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        y = L.serve(x)
+    L.serve(real(rng(20).standard_normal((5000, 384)), "bfloat16")[0])
+    junk = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (1024, 16384, 17408, 32768, 1 << 16)]     # (whatever was freed)
+    for _ in range(2):
+        graph.replay()
+        assert torch.equal(y, L.serve(x)) and bool(torch.isfinite(y).all())
+        w.mul_(-1.5)
+        L.quantise()
+    assert all(bool((t == 255).all()) for t in junk) and L.status() == 0
+
+
+def test_a_failed_call_of_a_step_is_not_forgotten(B):
+    """Every call of a step has a status word of its own, which a later call does not clear."""
+    import torch
+    st, x, dh = make(40, 128, 2, 0.1)
+    st.forward(x); st.backward(dh)
+    assert st.status() == 0
+    space = st.space.get()
+    for k in range(st.space.words):
+        word = space[256 * k:256 * k + 4].view(torch.int32)
+        word[0] = -6
+        assert st.status() == -6
+        if k <= 2: st.backward(dh)                                # (the forward's words)
+        assert st.status() == -6
+        st.forward(x); st.backward(dh)
+        assert st.status() == 0
+    lin = st.linears[0]
+    for k in range(3):
+        lin.space.at(k)[:4].view(torch.int32)[0] = -6
+        assert st.status() == -6
+        st.forward(x); st.backward(dh)
+        assert st.status() == 0
+
+
 def test_empty_and_tiny_extents(B):
     import torch
     q, s = B.qbp_quantize_f8(torch.randn(32, 64, device="cuda"))
@@ -213,7 +259,9 @@ def test_empty_and_tiny_extents(B):
     e = torch.empty(0, 96, device="cuda")
     d = B.resnorm_desc(e, e)
     g = torch.ones(96, device="cuda")
-    r, h, q1, q2 = B.qbp_resnorm_fwd(d, e, e, g, g, g)
+    ws = torch.full((512,), 255, dtype=torch.uint8, device="cuda")
+    r, h, q1, q2 = B.qbp_resnorm_fwd(d, e, e, g, g, g, ws=ws)
+    assert B.status_word(ws) == 0                                 # (cleared where there is nothing to do, too)
     dx, db, dw1, dg, dw2 = B.qbp_resnorm_bwd(d, e, e, e, r, q1, q2, g, g, g)
     assert h.shape == (0, 96) and not dw1.any() and not dg.any() and not dw2.any()
     assert B.qbp_dropout(e, 0.5, 1).shape == (0, 96)
