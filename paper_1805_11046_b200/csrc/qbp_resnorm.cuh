@@ -322,15 +322,18 @@ static inline size_t join_ring(const qbp_resnorm_desc *d, const JoinShape &s, in
     const size_t slots = tensors == 1 ? kJoinSlots : kJoinBackSlots;
     return slots * (size_t)(s.warp ? kJoinWarpRows : 1) * (size_t)tensors * (join_section<false>((uint32_t)(d->cols * dtype_size(d->x_dtype))) + join_section<false>((uint32_t)(d->cols * dtype_size(d->b_dtype))));
 }
-// A thread takes sixteen columns, eight where the rings of two blocks would not fit an SM or where rows off the 16-byte boundaries go backwards
-// (whose addresses would not fit the registers beside sixteen columns' sums), and 32 (without a ring) beyond 8192.
+// A thread takes sixteen columns, and 32 (without a ring) beyond 8192.  It takes eight where the rings of two blocks would not fit an SM, and
+// backwards up to 2048 columns, for few rows (a row's chain is shorter: 2000 x 2048 bf16 29 us, with sixteen 37; 2000 x 4096 43 and 50; 30000 x
+// 2048 196 and 210, but 16384 x 4096 251 and 247) and for rows off the 16-byte boundaries, whose addresses do not fit the registers beside
+// sixteen columns' sums.
 static inline JoinShape join_shape(const qbp_resnorm_desc *d, int tensors, bool vec)
 {
     const int chunks = (int)((d->cols + 255) / 256);                 // a warp's eight columns a lane
     if (chunks <= 1) return {1, 32 * kJoinWarpRows, true};
     if (chunks <= 2) return {2, 32 * kJoinWarpRows, true};
     JoinShape s{2, 32 * ((chunks + 1) / 2), false};
-    if (chunks <= 16 && ((!vec && tensors == 2) || (s.threads > 128 && 2 * join_ring(d, s, tensors) > kJoinSmRings))) s = {1, 32 * chunks, false};
+    const bool short_chain = tensors == 2 && (!vec || chunks <= 8 || d->rows < 32ll * sm_count());
+    if (chunks <= 16 && (short_chain || (s.threads > 128 && 2 * join_ring(d, s, tensors) > kJoinSmRings))) s = {1, 32 * chunks, false};
     if (s.threads <= 512 && join_ring(d, s, tensors) <= kJoinMaxRing) return s;
     return {4, 32 * ((chunks + 3) / 4), false};
 }
