@@ -171,8 +171,8 @@ __device__ __forceinline__ ItemRows item_rows(const JoinItems &it, int64_t item)
 }
 
 // ---- rows through the ring -----------------------------------------------------------------------------------------------
-// A row is copied by a lane of its group's first warp, whose bytes a slot's barrier reports (full).  Forward a slot is free for the next
-// copy once its row's sums have been exchanged; backwards, where a row is read behind the exchange too, each warp says so (empty).  Every wait
+// A row is copied by a lane of its group's first warp, whose bytes a slot's barrier reports (full).  A slot is free for the next copy once
+// its row's sums have been exchanged; backwards with sixteen columns a thread, where a row is read behind the exchange too, each warp says so (empty).  Every wait
 // is bounded: a warp whose wait ran out raises the status word, gives copies in flight another millisecond, copies and waits for nothing any
 // more and goes through the rest of its rows for the block's barriers' sake.
 template <typename T> struct Pieces { static constexpr int n = sizeof(T) / 2; };
@@ -315,37 +315,33 @@ constexpr int kJoinWide = 4;                         // times eight columns a th
 
 // ================================================================= host side
 struct JoinShape { int ch, threads; bool warp; };
-constexpr size_t kJoinMaxRing = 200 * 1024, kJoinSmRings = 222 * 1024;        // of a block, of an SM
+constexpr size_t kJoinMaxRing = 200 * 1024;         // of a block
 // Shared memory of a block's ring: forward slots of one tensor of each type, backwards of two.
 static inline size_t join_ring(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
 {
-    const size_t slots = tensors == 1 ? kJoinSlots : kJoinBackSlots;
+    const size_t slots = tensors == 1 || s.ch == 1 ? kJoinSlots : kJoinBackSlots;
     return slots * (size_t)(s.warp ? kJoinWarpRows : 1) * (size_t)tensors * (join_section<false>((uint32_t)(d->cols * dtype_size(d->x_dtype))) + join_section<false>((uint32_t)(d->cols * dtype_size(d->b_dtype))));
 }
-// A thread takes sixteen columns, and 32 (without a ring) beyond 8192.  It takes eight where the rings of two blocks would not fit an SM, and
-// backwards up to 2048 columns, for few rows (a row's chain is shorter: 2000 x 2048 bf16 29 us, with sixteen 37; 2000 x 4096 43 and 50; 30000 x
-// 2048 196 and 210, but 16384 x 4096 251 and 247) and for rows off the 16-byte boundaries, whose addresses do not fit the registers beside
-// sixteen columns' sums.
-static inline JoinShape join_shape(const qbp_resnorm_desc *d, int tensors, bool vec)
+// Forward a thread takes sixteen columns.  Backwards it takes eight up to 4096 columns: a row's values then stay in registers behind the
+// exchange of its sums, and its slot is free at once (16384 x 4096 232 us, with sixteen 247; 2000 x 2048 bf16 28 and 37).  32 (without a ring)
+// beyond 8192.
+static inline JoinShape join_shape(const qbp_resnorm_desc *d, int tensors)
 {
     const int chunks = (int)((d->cols + 255) / 256);                 // a warp's eight columns a lane
-    if (chunks <= 1) return {1, 32 * kJoinWarpRows, true};
-    if (chunks <= 2) return {2, 32 * kJoinWarpRows, true};
-    JoinShape s{2, 32 * ((chunks + 1) / 2), false};
-    const bool short_chain = tensors == 2 && (!vec || chunks <= 8 || d->rows < 32ll * sm_count());
-    if (chunks <= 16 && (short_chain || (s.threads > 128 && 2 * join_ring(d, s, tensors) > kJoinSmRings))) s = {1, 32 * chunks, false};
+    if (chunks <= 2) return {chunks, 32 * kJoinWarpRows, true};
+    const JoinShape s = tensors == 2 && chunks <= 16 ? JoinShape{1, 32 * chunks, false} : JoinShape{2, 32 * ((chunks + 1) / 2), false};
     if (s.threads <= 512 && join_ring(d, s, tensors) <= kJoinMaxRing) return s;
     return {4, 32 * ((chunks + 3) / 4), false};
 }
 
 // Runs `call` with the kernel's compile-time choices.
-#define QBP_FOR_JOIN(shape, CH, WARP, MAXT, call)                                                                             \
+#define QBP_FOR_JOIN(shape, backwards, CH, WARP, MAXT, call)                                                                  \
     do {                                                                                                                      \
         if ((shape).warp && (shape).ch == 1) { constexpr int CH = 1, MAXT = 256; constexpr bool WARP = true; call; }          \
         else if ((shape).warp) { constexpr int CH = 2, MAXT = 256; constexpr bool WARP = true; call; }                        \
-        else if ((shape).ch == 1) { constexpr int CH = 1, MAXT = 512; constexpr bool WARP = false; call; }                    \
-        else if ((shape).threads <= 256) { constexpr int CH = 2, MAXT = 256; constexpr bool WARP = false; call; }             \
-        else { constexpr int CH = 2, MAXT = 512; constexpr bool WARP = false; call; }                                         \
+        else if ((shape).ch == 1 || (!(backwards) && (shape).threads <= 256)) {                                               \
+            constexpr int CH = (backwards) ? 1 : 2, MAXT = (backwards) ? 512 : 256; constexpr bool WARP = false; call;        \
+        } else { constexpr int CH = 2, MAXT = 512; constexpr bool WARP = false; call; }                                       \
     } while (0)
 
 // Launches with the ring's shared memory.

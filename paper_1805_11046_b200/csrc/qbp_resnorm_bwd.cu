@@ -43,9 +43,11 @@ __device__ __forceinline__ void join_leave(const float (&a)[CH][8], float *out, 
 }
 
 template <typename TX, typename TB, int CH, bool WARP, int MAXT, bool VEC>
-__global__ void __launch_bounds__(MAXT, MAXT == 256 && !WARP ? 2 : 1)
+__global__ void __launch_bounds__(MAXT, 1)
 join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__ PhiloxKeys keys)
 {
+    constexpr bool kHold = CH == 1;                  // a row's values stay in registers behind the exchange, its slot is free with it
+    constexpr int kSlots = kHold ? kJoinSlots : kJoinBackSlots;
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float fold[WARP ? kJoinWarpRows * 256 * CH : 1];            // WARP: the warps' sums
     __shared__ JoinScratch scratch;
@@ -58,16 +60,16 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
     join_bars_init(bars, all_warps);
     pdl_wait();
     if (blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;          // (a wait gives up a second later at the earliest)
-    uint8_t *const slots = ring + (uint32_t)(sub * kJoinBackSlots) * slot_bytes;
+    uint8_t *const slots = ring + (uint32_t)(sub * kSlots) * slot_bytes;
     uint64_t *const full = bars.full[sub];
     const JoinSource src[4] = {{P.dr, row_x, 0u}, {P.pre ? P.r : nullptr, row_x, off_r}, {P.pre ? P.dh : nullptr, row_b, off_h}, {P.b, row_b, off_b}};
     bool dead = false;
     JoinPlace place{0u, 0u}, ahead{0u, 1u};          // of the row at hand, of the next row to be copied
     const auto fetch = [&](int64_t row) {
         if (WARP || warp == 0) {
-            if (!WARP) join_wait(&bars.empty[ahead.slot], ahead.ph, dead, P.status);
+            if (!WARP && !kHold) join_wait(&bars.empty[ahead.slot], ahead.ph, dead, P.status);
             if (!dead) join_copy<TX, TB, 2, VEC>(slots + ahead.slot * slot_bytes, &full[ahead.slot], src, row, P.it.rows);
-            ahead = ahead.next(kJoinBackSlots);
+            ahead = ahead.next(kSlots);
         }
     };
     In<VEC> in[CH];
@@ -89,14 +91,16 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
         }
 #pragma unroll
         for (int k = 0; k < CH; ++k) join_gains<VEC>(P.gate, P.post ? P.w_post : nullptr, rows.gate * cols, c0 + k * apart, cols, gw[k]);
-        if (rows.first + sub < rows.end) fetch(rows.first + sub);
+        // (kHold: all slots are free, the last rows' sums have been exchanged)
+        for (int k = 0; k < (kHold ? kSlots : 1); ++k)
+            if (rows.first + sub + k * subs < rows.end) fetch(rows.first + sub + k * subs);
         for (int64_t row = rows.first + sub; row < rows.end; row += subs) {
             const int64_t at = row * cols + c0;
             const float rstd1 = next1, rstd2 = next2;
             if (row + subs < rows.end) {
                 if (P.post) next1 = __ldg(P.rstd_post + row + subs);
                 if (P.pre) next2 = __ldg(P.rstd_pre + row + subs);
-                fetch(row + subs);
+                if (!kHold) fetch(row + subs);
             }
             join_wait(&full[place.slot], place.ph, dead, P.status);
             const uint8_t *const slot = slots + place.slot * slot_bytes;
@@ -109,17 +113,24 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
             // Both means from one exchange: the second, of v w_post b, is linear in the first, m, with R = (dr + dh w_pre rstd_pre) - r m.
             float sums[3] = {0.0f, 0.0f, 0.0f};
             uint32_t kept = 0;                        // which elements the dropout keeps, a bit each
+            float V[8], held_r[8], held_b[8];         // of eight columns: dr + dh w_pre rstd_pre, r, b
             {
 #pragma unroll
                 for (int k = 0; k < CH; ++k) {
                     float h[8], r[8], g[8], b[8];
                     get_h(k, h); get_r(k, r); get_g(k, g); get_b(k, b);
+                    if (kHold) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) { held_r[e] = r[e]; held_b[e] = b[e]; }
+                    }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         a_pre[k][e] = fmaf(h[e] * r[e], rstd2, a_pre[k][e]);
                         h[e] *= w2[k][e];
                         sums[0] = fmaf(h[e], r[e], sums[0]);
                         b[e] *= gw[k][e];
+                        g[e] = fmaf(h[e], rstd2, g[e]);
+                        if (kHold) V[e] = g[e];
                     }
                     if (P.drop) {
                         Kept<VEC> q;
@@ -130,13 +141,15 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
                     if (P.post) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
-                            sums[1] = fmaf(fmaf(h[e], rstd2, g[e]), b[e], sums[1]);
+                            sums[1] = fmaf(g[e], b[e], sums[1]);
                             sums[2] = fmaf(r[e], b[e], sums[2]);
                         }
                     }
                 }
             }
-            if (P.pre || P.post) { group_sums<WARP>(sums, scratch, half, warps); half ^= 1; }
+            if (kHold) __syncwarp();
+            if (kHold || P.pre || P.post) { group_sums<WARP>(sums, scratch, half, warps); half ^= 1; }
+            if (kHold && row + kSlots * subs < rows.end) fetch(row + kSlots * subs);
             // R = dr + rstd2 (dh w_pre) - r m2;  db = z rstd1 - b m1 with z = R dropout' gate w_post
             const float m2 = P.pre ? sums[0] * P.inv_cols * rstd2 * rstd2 * rstd2 : 0.0f;
             const float m1 = P.post ? (sums[1] - m2 * sums[2]) * factor * P.inv_cols * rstd1 * rstd1 * rstd1 : 0.0f;
@@ -145,8 +158,10 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
 #pragma unroll
                 for (int k = 0; k < CH; ++k) {
                     float R[8];
-                    get_g(k, R);
-                    if (P.pre) {
+                    if (kHold) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) R[e] = fmaf(-held_r[e], m2, V[e]);
+                    } else if (get_g(k, R); P.pre) {
                         float h[8], r[8];
                         get_h(k, h); get_r(k, r);
 #pragma unroll
@@ -154,7 +169,10 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
                     }
                     if (P.b) {
                         float b[8], z[8];
-                        get_b(k, b);
+                        if (kHold) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) b[e] = held_b[e];
+                        } else get_b(k, b);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) z[e] = R[e] * f1;
                         if (P.drop) {
@@ -181,9 +199,11 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
                     }
                 }
             }
-            __syncwarp();
-            if (!WARP && lane == 0) mbar_arrive(&bars.empty[place.slot]);
-            place = place.next(kJoinBackSlots);
+            if (!kHold) {
+                __syncwarp();
+                if (!WARP && lane == 0) mbar_arrive(&bars.empty[place.slot]);
+            }
+            place = place.next(kSlots);
         }
         if (P.sum_gate) join_leave<CH, WARP, VEC>(S, P.part_gate + item * cols, P.post ? P.w_post : nullptr, cols, c0, apart, false, fold, 32 * all_warps);
         if (P.sum_post)
@@ -368,9 +388,9 @@ __global__ void __launch_bounds__(32 * kSumHigh) join_sum_kernel(const __grid_co
 // ================================================================= host side
 // Partial rows of dgate: none where an item is all of a gate's rows, whose sum is the gradient.
 static size_t gate_parts(const JoinItems &it) { return it.splits > 1 ? (size_t)(it.gates * it.splits * it.cols) : 0; }
-static JoinCut join_cut_bwd(const qbp_resnorm_desc *d, bool per_gate, bool vec)
+static JoinCut join_cut_bwd(const qbp_resnorm_desc *d, bool per_gate)
 {
-    const JoinShape s = join_shape(d, 2, vec);
+    const JoinShape s = join_shape(d, 2);
     return join_cut(d, s, per_gate, join_blocks(d, s, 2), s.warp ? 2 : 4);
 }
 
@@ -378,11 +398,10 @@ extern "C" __attribute__((visibility("default"))) size_t qbp_resnorm_bwd_workspa
 {
     if (!d || d->rows <= 0 || d->cols <= 0) return 256;
     size_t most = 0;
-    for (bool per_gate : {false, true})
-        for (bool vec : {false, true}) {
-            const JoinCut c = join_cut_bwd(d, per_gate, vec);
-            most = std::max(most, 2 * align_up((size_t)(c.blocks * d->cols) * 4, 256) + align_up(gate_parts(c.it) * 4, 256));
-        }
+    for (bool per_gate : {false, true}) {
+        const JoinCut c = join_cut_bwd(d, per_gate);
+        most = std::max(most, 2 * align_up((size_t)(c.blocks * d->cols) * 4, 256) + align_up(gate_parts(c.it) * 4, 256));
+    }
     return 256 + most;
 }
 
@@ -414,7 +433,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
         return fail(QBP_ERR_WORKSPACE, "resnorm_bwd: workspace NULL, misaligned or smaller than %zu bytes", qbp_resnorm_bwd_workspace_bytes(d));
     const bool vec = d->cols % 8 == 0 && aligned16(dr) && aligned16(dh) && aligned16(b) && aligned16(r) && aligned16(dx) && aligned16(db) && aligned16(w_post) &&
                      aligned16(gate) && aligned16(w_pre);
-    const JoinCut c = join_cut_bwd(d, gate || dgate, vec);
+    const JoinCut c = join_cut_bwd(d, gate || dgate);
     WsCarver w(ws, ws_bytes);
     JoinBwdParams P{};
     P.status = w.take<int>(1);
@@ -431,10 +450,10 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
     P.drop = P.d.threshold == 65536u ? 2 : P.d.threshold ? 1 : 0;
     P.wide = aligned_to(dx, 32) && aligned_to(db, 32) ? 1 : 0;
     const PhiloxKeys keys = philox_keys_host(d->seed);
-    const JoinShape s = join_shape(d, 2, vec);
+    const JoinShape s = join_shape(d, 2);
     QBP_TRACE_BEGIN(st);
     if (s.ch <= 2)
-        QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, CH, WARP, MAXT, {
+        QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, true, CH, WARP, MAXT, {
             static PerDeviceOnce once[2];
             if ((rc = launch_join(vec ? join_bwd_kernel<TX, TB, CH, WARP, MAXT, true> : join_bwd_kernel<TX, TB, CH, WARP, MAXT, false>, once[vec], c.blocks, s, join_ring(d, s, 2), st, P, keys))) return rc;
         })));
