@@ -8,7 +8,7 @@ struct JoinParams {
     const void *x, *b; const float *w_post, *gate, *w_pre;
     void *r, *h; float *rstd_post, *rstd_pre;
     float eps, alpha, inv_cols;
-    int post, pre, drop, x_dtype, b_dtype, wide;      // wide: outputs of fp32 start on 32-byte boundaries
+    int post, pre, drop, x_dtype, b_dtype, slots, wide;      // wide: outputs of fp32 start on 32-byte boundaries
     int *status;
     DropoutParams d;
 };
@@ -27,7 +27,8 @@ join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ Ph
     join_bars_init(bars, all_warps);
     pdl_wait();
     if (blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;          // (a wait gives up a second later at the earliest)
-    uint8_t *const slots = ring + (uint32_t)(sub * kJoinSlots) * slot_bytes;
+    const uint32_t n_slots = (uint32_t)P.slots;
+    uint8_t *const slots = ring + (uint32_t)sub * n_slots * slot_bytes;
     uint64_t *const full = bars.full[sub];
     const JoinSource src[2] = {{P.x, row_x, 0u}, {P.b, row_b, off_b}};
     bool dead = false;
@@ -68,7 +69,7 @@ join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ Ph
         }
         // (all slots are free: the last rows' sums have been exchanged)
         JoinPlace p = place;
-        for (int k = 0; k < kJoinSlots; ++k) { fetch(rows.first + sub + k * subs, rows.end, p.slot); p = p.next(kJoinSlots); }
+        for (uint32_t k = 0; k < n_slots; ++k) { fetch(rows.first + sub + k * subs, rows.end, p.slot); p = p.next(n_slots); }
         float rstd = 1.0f;
         if (rows.first + sub < rows.end) {
             join_wait(&full[place.slot], place.ph, dead, P.status);
@@ -103,7 +104,7 @@ join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ Ph
                     for (int e = 0; e < 8; ++e) sums[0] = fmaf(r[k][e], r[k][e], sums[0]);    // (zero behind the last column, as x and b are)
                 }
             }
-            const JoinPlace following = place.next(kJoinSlots);
+            const JoinPlace following = place.next(n_slots);
             if (row + subs < rows.end) {
                 join_wait(&full[following.slot], following.ph, dead, P.status);
                 if (P.post) sums[1] = square_sum(following.slot, row + subs);
@@ -111,7 +112,7 @@ join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ Ph
             __syncwarp();
             group_sums<WARP>(sums, scratch, half, warps);
             half ^= 1;
-            fetch(row + kJoinSlots * subs, rows.end, place.slot);
+            fetch(row + (int64_t)n_slots * subs, rows.end, place.slot);
             place = following;
             rstd = P.post ? rsqrtf(sums[1] * P.inv_cols + P.eps) : 1.0f;
             if (P.pre) {
@@ -242,6 +243,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_fwd(const qbp_
     P.d = dropout_params(d->p, d->tensor_id, d->index_base);
     P.drop = P.d.threshold == 65536u ? 2 : P.d.threshold ? 1 : 0;
     P.status = static_cast<int *>(ws);
+    P.slots = join_slots(d, s, 1);
     P.wide = aligned_to(r, 32) && aligned_to(h, 32) ? 1 : 0;
     const PhiloxKeys keys = philox_keys_host(d->seed);
     QBP_TRACE_BEGIN(st);

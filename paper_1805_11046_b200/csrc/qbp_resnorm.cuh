@@ -1,14 +1,14 @@
-// The join between two blocks of a residual network and its gradients (qbp_resnorm_fwd in qbp_resnorm.cu, qbp_resnorm_bwd in
-// qbp_resnorm_bwd.cu; include/qbp.h): what both use.  Norm after a
-// block, gate, dropout, residual stream and the norm before the next block, in one pass over the rows.
+// The join between two blocks of a residual network and its gradients (include/qbp.h; qbp_resnorm_fwd in qbp_resnorm.cu, qbp_resnorm_bwd in
+// qbp_resnorm_bwd.cu): what both use.  Norm after a block, gate, dropout, residual stream and the norm before the next block, in one pass over
+// the rows.
 //
-// A row is held in registers by the threads of one group: a warp (of a block's eight) for rows of up to 512 columns, a block of
-// up to 512 threads beyond; a thread has CH times eight columns.  The two sums over a row (of b^2 and of r^2; backwards of the
-// gradients' projections on r and b) are exchanged between the group's threads, forward a row's second with the next row's first, backwards
-// both at once, and nothing is read twice.  A block
-// takes neighbouring rows of one gate (an item) and keeps the parameters of its columns in registers.  Rows come through a ring of two
-// or three in shared memory, copied whole by one thread (cp.async.bulk): a row is on its way while the one before is worked on, and stays
-// out of the threads' registers.  (Copied by the threads that read it, 16 bytes each, a row of 48 KB took 2100 cycles of their time, of 5900.)
+// A row is held in registers by the threads of one group: a warp (of a block's eight) for rows of up to 512 columns, a block of up to 512
+// threads beyond; a thread has CH times eight columns.  The two sums over a row (of b^2 and of r^2; backwards of the gradients' projections on
+// r and b) are exchanged between the group's threads, forward a row's second with the next row's first, backwards both at once, and nothing
+// is read from memory twice.  A block takes neighbouring rows of one gate (an item) and keeps the parameters of its columns in registers.  Rows
+// come through a ring of two or three in shared memory, copied whole by one thread (cp.async.bulk): a row is on its way while the one before is
+// worked on, and stays out of the threads' registers.  (Copied by the threads that read it, 16 bytes each, a row of 48 KB took 2100 cycles of
+// their time, of 5900.)  16384 x 4096, fp32 stream, bf16 blocks, dropout: forward 142 us, 5.7 TB/s, backward 204 us, 5.9 TB/s.
 //
 // Backwards, with gate and w_post constant along an item's columns, dw_post and dgate are multiples of one sum over its rows,
 // S = sum of R dropout'(b rstd_post): dgate = w_post S, dw_post = gate S.  A thread keeps S and dw_pre's sum in registers, a block leaves
@@ -316,12 +316,21 @@ constexpr int kJoinWide = 4;                         // times eight columns a th
 // ================================================================= host side
 struct JoinShape { int ch, threads; bool warp; };
 constexpr size_t kJoinMaxRing = 200 * 1024;         // of a block
-// Shared memory of a block's ring: forward slots of one tensor of each type, backwards of two.
-static inline size_t join_ring(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
+static inline size_t join_slot(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
 {
-    const size_t slots = tensors == 1 || s.ch == 1 ? kJoinSlots : kJoinBackSlots;
-    return slots * (size_t)(s.warp ? kJoinWarpRows : 1) * (size_t)tensors * (join_section<false>((uint32_t)(d->cols * dtype_size(d->x_dtype))) + join_section<false>((uint32_t)(d->cols * dtype_size(d->b_dtype))));
+    return (size_t)(s.warp ? kJoinWarpRows : 1) * (size_t)tensors * (join_section<false>((uint32_t)(d->cols * dtype_size(d->x_dtype))) + join_section<false>((uint32_t)(d->cols * dtype_size(d->b_dtype))));
 }
+// Blocks that an SM has threads for (16 warps, which their registers allow; 8 backwards where a row is a warp's).
+static inline int join_per_sm(const JoinShape &s, int tensors) { return s.ch > 2 ? 1 : std::max((s.warp && tensors == 2 ? 256 : 512) / s.threads, 1); }
+// Slots of a block's ring (forward of one tensor of each type, backwards of two): three, but two where an SM's blocks would ask for more
+// than 112 KB at a time (fp32 stream, bf16 blocks, us with three and two: 30000 x 2048 forward 136 and 123, backward 208 and 182; with less, 16384 x
+// 4096 bf16 forward 93 and 114; one block an SM, 8192 x 8192 134 and 149).
+static inline int join_slots(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
+{
+    if (tensors == 2 && s.ch != 1) return kJoinBackSlots;
+    return join_per_sm(s, tensors) == 1 || 3 * join_slot(d, s, tensors) * (size_t)join_per_sm(s, tensors) <= 112 * 1024 ? kJoinSlots : kJoinSlots - 1;
+}
+static inline size_t join_ring(const qbp_resnorm_desc *d, const JoinShape &s, int tensors) { return (size_t)join_slots(d, s, tensors) * join_slot(d, s, tensors); }
 // Forward a thread takes sixteen columns.  Backwards it takes eight up to 4096 columns: a row's values then stay in registers behind the
 // exchange of its sums, and its slot is free at once (16384 x 4096 232 us, with sixteen 247; 2000 x 2048 bf16 28 and 37).  32 (without a ring)
 // beyond 8192.
@@ -392,11 +401,11 @@ static inline JoinCut join_cut(const qbp_resnorm_desc *d, const JoinShape &s, bo
     c.blocks = std::min(most, it.gates * it.splits);
     return c;
 }
-// Blocks of a wave: 16 warps an SM (8 backwards where a row is a warp's), which their registers allow, or what their rings leave room for.
+// Blocks of a wave, or as many of an SM's as their rings leave room for.
 static inline int64_t join_blocks(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
 {
-    const int64_t per_sm = s.ch > 2 ? 1 : std::min<int64_t>((s.warp && tensors == 2 ? 256 : 512) / s.threads, (int64_t)(227 * 1024 / (join_ring(d, s, tensors) + 2048 + (s.warp && tensors == 2 ? 16384 : 0))));
-    return (int64_t)sm_count() * std::max<int64_t>(per_sm, 1);
+    const int64_t room = s.ch > 2 ? 1 : (int64_t)(227 * 1024 / (join_ring(d, s, tensors) + 2048 + (s.warp && tensors == 2 ? 16384 : 0)));
+    return (int64_t)sm_count() * std::max<int64_t>(std::min<int64_t>(join_per_sm(s, tensors), room), 1);
 }
 
 }  // namespace qbp

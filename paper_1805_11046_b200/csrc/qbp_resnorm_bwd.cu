@@ -8,7 +8,7 @@ struct JoinBwdParams {
     const void *dr, *dh, *b, *r; const float *rstd_post, *rstd_pre, *w_post, *gate, *w_pre;
     void *dx, *db; float *part_post, *part_gate, *part_pre;
     float alpha, inv_cols;
-    int post, pre, drop, x_dtype, b_dtype, wide, sum_post, sum_gate, sum_pre;
+    int post, pre, drop, x_dtype, b_dtype, slots, wide, sum_post, sum_gate, sum_pre;
     int *status;
     DropoutParams d;
 };
@@ -47,7 +47,6 @@ __global__ void __launch_bounds__(MAXT, 1)
 join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__ PhiloxKeys keys)
 {
     constexpr bool kHold = CH == 1;                  // a row's values stay in registers behind the exchange, its slot is free with it
-    constexpr int kSlots = kHold ? kJoinSlots : kJoinBackSlots;
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float fold[WARP ? kJoinWarpRows * 256 * CH : 1];            // WARP: the warps' sums
     __shared__ JoinScratch scratch;
@@ -60,7 +59,8 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
     join_bars_init(bars, all_warps);
     pdl_wait();
     if (blockIdx.x == 0 && threadIdx.x == 0) *P.status = 0;          // (a wait gives up a second later at the earliest)
-    uint8_t *const slots = ring + (uint32_t)(sub * kSlots) * slot_bytes;
+    const uint32_t n_slots = kHold ? (uint32_t)P.slots : (uint32_t)kJoinBackSlots;
+    uint8_t *const slots = ring + (uint32_t)sub * n_slots * slot_bytes;
     uint64_t *const full = bars.full[sub];
     const JoinSource src[4] = {{P.dr, row_x, 0u}, {P.pre ? P.r : nullptr, row_x, off_r}, {P.pre ? P.dh : nullptr, row_b, off_h}, {P.b, row_b, off_b}};
     bool dead = false;
@@ -69,7 +69,7 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
         if (WARP || warp == 0) {
             if (!WARP && !kHold) join_wait(&bars.empty[ahead.slot], ahead.ph, dead, P.status);
             if (!dead) join_copy<TX, TB, 2, VEC>(slots + ahead.slot * slot_bytes, &full[ahead.slot], src, row, P.it.rows);
-            ahead = ahead.next(kSlots);
+            ahead = ahead.next(n_slots);
         }
     };
     In<VEC> in[CH];
@@ -92,8 +92,8 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
 #pragma unroll
         for (int k = 0; k < CH; ++k) join_gains<VEC>(P.gate, P.post ? P.w_post : nullptr, rows.gate * cols, c0 + k * apart, cols, gw[k]);
         // (kHold: all slots are free, the last rows' sums have been exchanged)
-        for (int k = 0; k < (kHold ? kSlots : 1); ++k)
-            if (rows.first + sub + k * subs < rows.end) fetch(rows.first + sub + k * subs);
+        for (uint32_t k = 0; k < (kHold ? n_slots : 1u); ++k)
+            if (rows.first + sub + (int64_t)k * subs < rows.end) fetch(rows.first + sub + (int64_t)k * subs);
         for (int64_t row = rows.first + sub; row < rows.end; row += subs) {
             const int64_t at = row * cols + c0;
             const float rstd1 = next1, rstd2 = next2;
@@ -149,7 +149,7 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
             }
             if (kHold) __syncwarp();
             if (kHold || P.pre || P.post) { group_sums<WARP>(sums, scratch, half, warps); half ^= 1; }
-            if (kHold && row + kSlots * subs < rows.end) fetch(row + kSlots * subs);
+            if (kHold && row + (int64_t)n_slots * subs < rows.end) fetch(row + (int64_t)n_slots * subs);
             // R = dr + rstd2 (dh w_pre) - r m2;  db = z rstd1 - b m1 with z = R dropout' gate w_post
             const float m2 = P.pre ? sums[0] * P.inv_cols * rstd2 * rstd2 * rstd2 : 0.0f;
             const float m1 = P.post ? (sums[1] - m2 * sums[2]) * factor * P.inv_cols * rstd1 * rstd1 * rstd1 : 0.0f;
@@ -203,7 +203,7 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
                 __syncwarp();
                 if (!WARP && lane == 0) mbar_arrive(&bars.empty[place.slot]);
             }
-            place = place.next(kSlots);
+            place = place.next(n_slots);
         }
         if (P.sum_gate) join_leave<CH, WARP, VEC>(S, P.part_gate + item * cols, P.post ? P.w_post : nullptr, cols, c0, apart, false, fold, 32 * all_warps);
         if (P.sum_post)
@@ -433,6 +433,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
         return fail(QBP_ERR_WORKSPACE, "resnorm_bwd: workspace NULL, misaligned or smaller than %zu bytes", qbp_resnorm_bwd_workspace_bytes(d));
     const bool vec = d->cols % 8 == 0 && aligned16(dr) && aligned16(dh) && aligned16(b) && aligned16(r) && aligned16(dx) && aligned16(db) && aligned16(w_post) &&
                      aligned16(gate) && aligned16(w_pre);
+    const JoinShape s = join_shape(d, 2);
     const JoinCut c = join_cut_bwd(d, gate || dgate);
     WsCarver w(ws, ws_bytes);
     JoinBwdParams P{};
@@ -448,9 +449,9 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
     if (dw_pre && c.blocks == 1) P.part_pre = dw_pre;
     P.d = dropout_params(d->p, d->tensor_id, d->index_base);
     P.drop = P.d.threshold == 65536u ? 2 : P.d.threshold ? 1 : 0;
+    P.slots = join_slots(d, s, 2);
     P.wide = aligned_to(dx, 32) && aligned_to(db, 32) ? 1 : 0;
     const PhiloxKeys keys = philox_keys_host(d->seed);
-    const JoinShape s = join_shape(d, 2);
     QBP_TRACE_BEGIN(st);
     if (s.ch <= 2)
         QBP_FOR_DTYPE(d->x_dtype, TX, QBP_FOR_DTYPE(d->b_dtype, TB, QBP_FOR_JOIN(s, true, CH, WARP, MAXT, {
