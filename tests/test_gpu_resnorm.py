@@ -115,6 +115,30 @@ def test_join_and_gradients(B, rows, cols, stream, dtype):
     check(B, rows, cols, stream, dtype, gate_rows=0, p=0.2, alpha=0.75)
 
 
+# rows off the 16-byte boundaries in every kind of group, enough of them for a block to take several; rows shorter than 32 bytes; the last
+# lanes' columns missing
+@pytest.mark.parametrize("rows,cols", [(4000, 3), (5000, 13), (3000, 201), (3000, 333), (1300, 513), (1300, 1001), (1000, 2047), (700, 3331), (700, 4095), (500, 5003), (400, 8191)])
+@pytest.mark.parametrize("stream,dtype", [("float32", "bfloat16"), ("bfloat16", "bfloat16"), ("float32", "float32"), ("float16", "float32")])
+def test_rows_off_the_16_byte_boundaries(B, rows, cols, stream, dtype):
+    check(B, rows, cols, stream, dtype, gate_rows=[0, rows // 3, 1][rows // 100 % 3] if cols < 3000 else 0, p=0.1 if cols % 4 == 1 else 0.0, alpha=0.5)
+
+
+@pytest.mark.parametrize("cols", [7, 333, 1001, 4095])
+def test_outputs_over_inputs_off_the_16_byte_boundaries(B, cols):
+    """A row's copy takes bytes of the rows beside it, which another block may be writing: they count for nothing."""
+    import torch
+    i = inputs(2500, cols, "float32", "bfloat16", 1, 4)
+    x, b, dr, dh = (i[k][0] for k in ("x", "b", "dr", "dh"))
+    d = B.resnorm_desc(x, b, alpha=0.5, eps=EPS, p=0.2, seed=3)
+    r, h, q1, q2 = B.qbp_resnorm_fwd(d, x, b, i["w1"][0], i["gate"][0], i["w2"][0])
+    want = B.qbp_resnorm_bwd(d, dr, dh, b, r, q1, q2, i["w1"][0], i["gate"][0], i["w2"][0])
+    x2, b2, dr2, dh2 = x.clone(), b.clone(), dr.clone(), dh.clone()
+    got = B.qbp_resnorm_fwd(d, x2, b2, i["w1"][0], i["gate"][0], i["w2"][0], r=x2, h=b2)
+    assert all(torch.equal(u, v) for u, v in zip(got, (r, h, q1, q2)))
+    got = B.qbp_resnorm_bwd(d, dr2, dh2, b, r, q1, q2, i["w1"][0], i["gate"][0], i["w2"][0], dx=dr2, db=dh2)
+    assert all(torch.equal(u, v) for u, v in zip(got, want))
+
+
 @pytest.mark.parametrize("rows,cols,gate_rows", [(1, 64, 1), (10, 64, 1), (10, 200, 3), (333 * 3, 1000, 333), (1000, 48, 7), (50, 2056, 20), (600, 1536, 600), (601, 1536, 600), (4, 16384, 2)])
 def test_gates_of_groups_of_rows(B, rows, cols, gate_rows):
     check(B, rows, cols, "float32", "bfloat16", gate_rows=gate_rows, p=0.0, alpha=1.0)
