@@ -278,17 +278,18 @@ template <typename T> __device__ __forceinline__ void split_add(void *out, int64
 }
 
 // Warps 2..9: the blocks kb0..kb1 of all rows (at most kSplitQuantise) to e4m3, into the stages as the product wants them: rows of 128 bytes,
-// 16-byte pieces swizzled by the row, and each row's scale byte at its place in a piece.  Every eighth block is a warp's (with all warps on
-// one block, one block after the other, a block took half a microsecond, nearly all of it latency), two rows at a time, sixteen lanes to a
-// row, all rows' loads on their way at once.  False when a wait ran out.
+// 16-byte pieces swizzled by the row, and each row's scale byte at its place in a piece.  A block is a warp's (with all warps on one
+// block, one block after the other, a block took half a microsecond, nearly all of it latency), two rows at a time, sixteen lanes to a row, all
+// rows' loads on their way at once.  No more warps than stages take part: a stage is then written at most a round after the warp's own last
+// block, and the parity of its barrier tells whether that round is free; for a stage further ahead, the round before the last would pass for
+// it.  False when a wait ran out.
 template <typename T>
 __device__ __forceinline__ bool split_quantise(const F8SplitParams &P, uint8_t *smem, uint64_t *full_bar, uint64_t *empty_bar, int kb0, int kb1)
 {
     const int lane = threadIdx.x & 31, lane16 = lane & 15, high = lane >> 4;
-    const int M = (int)P.M, first = kb0 + (int)(threadIdx.x >> 5) - 2;
-    uint32_t s = (uint32_t)(first - kb0), ph = 1;
-    while (s >= (uint32_t)P.stages) { s -= (uint32_t)P.stages; ph ^= 1u; }
-    for (int kb = first; kb < kb1; kb += 8) {
+    const int M = (int)P.M, warps = min(8, P.stages), me = (int)(threadIdx.x >> 5) - 2;
+    uint32_t s = (uint32_t)me, ph = 1;
+    for (int kb = kb0 + me; me < warps && kb < kb1; kb += warps) {
         const int64_t c = 128ll * kb + 8 * lane16;
         const T *x = static_cast<const T *>(P.x) + (c < P.K ? c : 0);
         const auto load = [&](int r) { return load8(x + (r < M ? r : 0) * P.ld, r < M && c < P.K ? 8 : 0, P.vec != 0); };
@@ -318,8 +319,8 @@ __device__ __forceinline__ bool split_quantise(const F8SplitParams &P, uint8_t *
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) mbar_arrive(&full_bar[s]);
-        s += 8u;
-        while (s >= (uint32_t)P.stages) { s -= (uint32_t)P.stages; ph ^= 1u; }
+        s += (uint32_t)warps;
+        if (s >= (uint32_t)P.stages) { s -= (uint32_t)P.stages; ph ^= 1u; }
     }
     return true;
 }

@@ -260,6 +260,19 @@ def test_a_nan_enters_its_own_outputs_alone(B, M, N, K, transA, transB):
     assert torch.equal(torch.isnan(got), bad) and torch.equal(got[~bad], good[~bad])
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 32768, 4096), (16, 19200, 2560), (3, 24016, 1040), (9, 20000, 528), (2, 19072, 16384), (16, 8192, 16384)])
+def test_linear_of_more_features_than_a_wave(B, M, N, K):
+    """Two CTAs share an SM, each with a short ring that its quantising warps go round many times."""
+    import torch
+    x = torch.from_numpy(wide_values(M, K, M).astype(np.float32)).to(torch.bfloat16).cuda()
+    w = torch.randint(0, 120, (N, K), dtype=torch.uint8, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    sw = torch.full((B._scale_bytes(N, K),), 120, dtype=torch.uint8, device="cuda")
+    q, s = B.qbp_quantize_f8(x)
+    want = B.qbp_gemm_f8(q, s, w, sw, transB=True, out_dtype=x.dtype)
+    for _ in range(5): assert torch.equal(B.qbp_linear_f8(x, w, sw), want)
+    assert B.status_word(B.workspace(256)) == 0
+
+
 def test_small_products_of_many_streams(B):
     """Products in clusters that come to the SMs together: each has the tensor memory it needs, and the results are those of one at a time."""
     import torch
