@@ -203,7 +203,7 @@ static int launch_f8_quantize(const void *x, int dtype, int64_t rows, int64_t co
 // sums of these rows into its shared memory (reading them there took a round trip a row: 128 x 1024 x 512 22.6 us with the launch).
 //
 // Roles: warp 0 loads by TMA, warp 1 copies scales to tensor memory and issues the MMAs, warps 2..9 take the accumulator out.
-// Of a layer that serves few rows (TX: their type), warps 2..9 first quantise the rows, each CTA its part of the reduction, straight into
+// Of a layer that serves up to eight rows (TX: their type), warps 2..9 first quantise the rows, each CTA its part of the reduction, straight into
 // the stages, with the scales of one block at a time.
 // Every wait is bounded.
 constexpr int kSplitThreads = 320;
@@ -214,7 +214,7 @@ constexpr uint32_t kSplitSmem = 220u * 1024u;
 constexpr uint32_t kSplitCols = 256;             // tensor memory: the accumulator in [0, 128), then sets of 4 columns of scales:
 constexpr uint32_t kSplitSetU = 128, kSplitSetV = 144;
 constexpr int kSplitSets = 4, kSplitBlockSets = 16;      // of U (and of V from memory), a set for four blocks; of V quantised here, for one
-constexpr int64_t kSplitQuantise = 16;           // rows that every CTA quantises for itself, at most
+constexpr int64_t kSplitQuantise = 8;            // rows that every CTA quantises for itself, at most
 constexpr size_t kSplitClusterSmem = 116u * 1024u;
 
 struct F8SplitParams {
@@ -500,7 +500,9 @@ static int split_clusters(int parts)
         attr.val.clusterDim.x = (unsigned)parts; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
         cfg.attrs = &attr; cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, f8_split_kernel<FromCodes>, &cfg) != cudaSuccess) { cudaGetLastError(); n = sm_count() / parts * 3 / 4; }
+        // (asked before the first launch, which opts in to this much shared memory too)
+        if (cudaFuncSetAttribute(f8_split_kernel<FromCodes>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSplitSmem) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, f8_split_kernel<FromCodes>, &cfg) != cudaSuccess) { cudaGetLastError(); n = sm_count() / parts * 3 / 4; }
         if (dev < 0) return n;
         found[k][dev] = n;
         asked[k].mark(dev);
@@ -511,42 +513,64 @@ static int split_clusters(int parts)
 // Rows as real numbers, to be quantised on the way (x NULL: codes and scales are there).
 struct SplitInput { const void *x; int64_t ld; };
 
+// How a product is cut: tiles of 128 by bn outputs, each in `parts`, with rings of `stages`.
+struct SplitShape { int bn, k_blocks, parts, stages; int64_t tiles_n, tiles_m; uint32_t stage_bytes, sums_bytes; };
+static SplitShape split_shape(const F8Product &p)
+{
+    SplitShape P{};
+    P.bn = p.transA || p.M > 64 ? 128 : p.M > 32 ? 64 : p.M > 16 ? 32 : 16;
+    P.k_blocks = (int)f8_blocks(p.K);
+    P.tiles_n = f8_blocks(p.N); P.tiles_m = (p.M + P.bn - 1) / P.bn;
+    // Parts: as many as run at the same time, where they save more blocks of 0.25 us than adding up the tile's rows costs (one call of
+    // many in a row, one part and the best, us: 1 x 4096 x 4096 12.7 and 7.9 (four), 64 x 1024 x 1024 5.9 and 5.3 (eight), 128 x 1024 x
+    // 1024 6.4 and 6.7 (eight), 512 x 2048 x 4096 14.3 and 14.1 (two), x 8192 23.9 and 20.6).
+    P.parts = 1;
+    while (P.parts < kSplitMaxParts && 2 * P.parts <= P.k_blocks && P.tiles_n * P.tiles_m <= split_clusters(2 * P.parts)) P.parts *= 2;
+    if (P.k_blocks - (P.k_blocks + P.parts - 1) / P.parts <= 2 + P.bn / 16 * (P.parts == 2 ? 3 : 1)) P.parts = 1;
+    P.stage_bytes = (uint32_t)align_up(128u * (128u + (uint32_t)P.bn) + 2u * kF8Piece, 1024);
+    P.sums_bytes = P.parts > 1 ? (uint32_t)P.bn * 512u : 0u;
+    P.stages = (int)std::min<int64_t>(kSplitMaxStages, (kSplitSmem - 1024 - P.sums_bytes) / P.stage_bytes);
+    // more than a wave: two CTAs an SM, one's loads beside the other's epilogue
+    if (P.tiles_n * P.tiles_m > sm_count()) P.stages = std::min<int>(P.stages, (int)((kSplitSmem / 2 - 2048) / P.stage_bytes));
+    P.stages = std::min(P.stages, std::max(2, (P.k_blocks + P.parts - 1) / P.parts + 1));
+    P.stages -= P.stages % (int)kSplitRelease;
+    return P;
+}
+
+// Whether every CTA quantises the rows for itself, each warp some blocks one after the other, or a launch before does (one call of many in
+// a row, on the way and apart, us: 1 x 1024 x 1024 5.8 and 6.6, 2 x 32768 x 4096 26.1 and 27.3, 4 x 32768 x 4096 29.9 and 27.3, 4 x 8192 x 8192 18.4
+// and 19.0, 8 x 8192 x 8192 24.3 and 19.1, 8 x 4096 x 4096 9.5 and 9.4, 8 x 2048 x 8192 13.6 and 11.2, 16 x 4096 x 4096 11.0 and 9.5; a launch less is
+// 2.4 of the host's where it is the bound).
+static bool split_quantises(const F8Product &p)
+{
+    if (p.M > kSplitQuantise) return false;
+    const SplitShape s = split_shape(p);
+    const int blocks = (s.k_blocks + s.parts - 1) / s.parts, warps = std::min(8, s.stages), rounds = (blocks + warps - 1) / warps;
+    return p.M * p.M * rounds <= 64;
+}
+
 static int launch_f8_split(const F8Product &p, const SplitInput &in, cudaStream_t st)
 {
     F8SplitParams P{};
     int rc;
-    P.bn = p.transA || p.M > 64 ? 128 : p.M > 32 ? 64 : p.M > 16 ? 32 : 16;
+    static PerDeviceOnce configured;
+    QBP_SMEM_OPT_IN(configured, f8_split_kernel<FromCodes>, kSplitSmem);
+    const SplitShape s = split_shape(p);
+    P.bn = s.bn; P.k_blocks = s.k_blocks; P.parts = s.parts; P.stages = s.stages; P.stage_bytes = s.stage_bytes;
     if (p.transB) { P.u = layout_kmajor(128, 128);        rc = make_map_2d(&P.mapU, p.B, p.N, p.K, 128, 128); }
     else          { P.u = layout_mnmajor(128, 128, 1, 0); rc = make_map_2d(&P.mapU, p.B, p.K, p.N, 128, 128); }
     if (rc) return rc;
     if (p.transA) P.v = layout_mnmajor(128, 128, 1, 0);
     else          P.v = layout_kmajor((uint32_t)P.bn, 128);
     P.idesc = make_idesc_f8(p.formatB, p.formatA, P.u.major, P.v.major, 128, (uint32_t)P.bn);
-    P.k_blocks = (int)f8_blocks(p.K);
-    const int64_t tiles_n = f8_blocks(p.N), tiles_m = (p.M + P.bn - 1) / P.bn;
-    static PerDeviceOnce configured;
-    QBP_SMEM_OPT_IN(configured, f8_split_kernel<FromCodes>, kSplitSmem);
-    // Parts: as many as run at the same time, where they save more blocks of 0.25 us than adding up the tile's rows costs (one call of
-    // many in a row, one part and the best, us: 1 x 4096 x 4096 12.7 and 7.9 (four), 64 x 1024 x 1024 5.9 and 5.3 (eight), 128 x 1024 x
-    // 1024 6.4 and 6.7 (eight), 512 x 2048 x 4096 14.3 and 14.1 (two), x 8192 23.9 and 20.6).
-    P.parts = 1;
-    while (P.parts < kSplitMaxParts && 2 * P.parts <= P.k_blocks && tiles_n * tiles_m <= split_clusters(2 * P.parts)) P.parts *= 2;
-    if (P.k_blocks - (P.k_blocks + P.parts - 1) / P.parts <= 2 + P.bn / 16 * (P.parts == 2 ? 3 : 1)) P.parts = 1;
-    P.stage_bytes = (uint32_t)align_up(P.u.tile_bytes + P.v.tile_bytes + 2u * kF8Piece, 1024);
-    const uint32_t sums_bytes = P.parts > 1 ? (uint32_t)P.bn * 512u : 0u;
-    P.stages = (int)std::min<int64_t>(kSplitMaxStages, (kSplitSmem - 1024 - sums_bytes) / P.stage_bytes);
-    // more than a wave: two CTAs an SM, one's loads beside the other's epilogue
-    if (tiles_n * tiles_m > sm_count()) P.stages = std::min<int>(P.stages, (int)((kSplitSmem / 2 - 2048) / P.stage_bytes));
-    P.stages = std::min(P.stages, std::max(2, (P.k_blocks + P.parts - 1) / P.parts + 1));
-    P.stages -= P.stages % (int)kSplitRelease;
     static_assert(kSplitMaxStages + (int)kSplitRelease <= 4 * kSplitSets - 3 && kSplitMaxStages + (int)kSplitRelease < kSplitBlockSets &&
                   kSplitSetU + 4 * kSplitSets <= kSplitSetV && kSplitSetV + 4 * kSplitBlockSets <= kSplitCols, "a set of scales is written again while MMAs may read it");
     // A cluster's CTA has an SM to itself, as the pair kernels' have: where CTAs of two clusters shared one with a third that waits for their
     // tensor memory, while their peers wait for the third's on another SM, none would end.
-    const size_t smem = std::max<size_t>(1024 + (size_t)P.stages * P.stage_bytes + sums_bytes, P.parts > 1 ? kSplitClusterSmem : 0);
+    const size_t smem = std::max<size_t>(1024 + (size_t)P.stages * P.stage_bytes + s.sums_bytes, P.parts > 1 ? kSplitClusterSmem : 0);
     P.M = p.M; P.N = p.N; P.out = p.out; P.dtype = p.dtype; P.status = p.status;
     P.su = p.sB; P.groups = f8_groups(p.K);
-    const dim3 grid((unsigned)(tiles_n * P.parts), (unsigned)tiles_m);
+    const dim3 grid((unsigned)(s.tiles_n * P.parts), (unsigned)s.tiles_m);
     if (in.x) {
         P.x = in.x; P.ld = in.ld; P.K = p.K;
         P.vec = aligned16(in.x) && in.ld * (int64_t)dtype_size(p.dtype) % 16 == 0 ? 1 : 0;
@@ -687,9 +711,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_linear_f8(const void *
         return QBP_OK;
     }
     if (!w || !sw || !aligned16(w) || !aligned16(sw)) return fail(QBP_ERR_INVALID_ARG, "linear_f8: the weights or their scales are NULL or not on a 16-byte boundary");
-    // Few rows are quantised by every CTA for itself (one call of many in a row, the quantiser apart and on the way, us: 1 x 4096 x 4096 11.5
-    // and 8.4, 16 x 1024 x 1024 8.1 and 7.1, 1 x 8192 x 8192 20.2 and 17.4; 32 x 1024 x 1024 8.3 and 9.2)
-    if (M <= kSplitQuantise) return launch_f8_split(p, SplitInput{x, ld}, st);
+    if (split_quantises(p)) return launch_f8_split(p, SplitInput{x, ld}, st);
     WsCarver c(ws, ws_bytes);
     c.take<int>(1);
     uint8_t *q = c.take<uint8_t>((size_t)M * (size_t)K), *s = c.take<uint8_t>(qbp_f8_scale_bytes(M, K));

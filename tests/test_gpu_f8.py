@@ -260,9 +260,10 @@ def test_a_nan_enters_its_own_outputs_alone(B, M, N, K, transA, transB):
     assert torch.equal(torch.isnan(got), bad) and torch.equal(got[~bad], good[~bad])
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 32768, 4096), (16, 19200, 2560), (3, 24016, 1040), (9, 20000, 528), (2, 19072, 16384), (16, 8192, 16384)])
-def test_linear_of_more_features_than_a_wave(B, M, N, K):
-    """Two CTAs share an SM, each with a short ring that its quantising warps go round many times."""
+@pytest.mark.parametrize("M,N,K", [(1, 32768, 4096), (2, 32768, 4096), (16, 19200, 2560), (3, 24016, 1040), (9, 20000, 528), (1, 19072, 16384), (16, 8192, 16384), (4, 8192, 8192), (8, 4096, 4096),
+                                   (5, 512, 1024), (8, 20000, 256), (7, 144, 400)])
+def test_linear_of_few_rows_and_many_features(B, M, N, K):
+    """More tiles than SMs: two CTAs share one, each with a short ring that its quantising warps go round many times."""
     import torch
     x = torch.from_numpy(wide_values(M, K, M).astype(np.float32)).to(torch.bfloat16).cuda()
     w = torch.randint(0, 120, (N, K), dtype=torch.uint8, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
