@@ -363,12 +363,17 @@ static int launch_join(void (*kernel)(Params, PhiloxKeys), PerDeviceOnce &once, 
     return QBP_OK;
 }
 
+// Whether rows, columns and gate_rows are such that no count made of them overflows (2^60 elements at most).
+static inline bool join_extents_ok(const qbp_resnorm_desc *d)
+{
+    return d->rows >= 0 && d->cols >= 0 && d->gate_rows >= 0 && d->cols <= kJoinMaxCols && d->rows <= ((int64_t)1 << 60) / std::max<int64_t>(d->cols, 1);
+}
 static inline int check_join(const qbp_resnorm_desc *d, const char *name, const void *b, const float *gate, const float *w_post, const float *w_pre)
 {
     if (!d) return fail(QBP_ERR_INVALID_ARG, "%s: NULL descriptor", name);
     if (!dtype_ok(d->x_dtype) || !dtype_ok(d->b_dtype)) return fail(QBP_ERR_INVALID_ARG, "%s: dtypes %d and %d", name, d->x_dtype, d->b_dtype);
     if (d->rows < 0 || d->cols < 0 || d->gate_rows < 0) return fail(QBP_ERR_INVALID_ARG, "%s: rows %lld, cols %lld, gate_rows %lld", name, (long long)d->rows, (long long)d->cols, (long long)d->gate_rows);
-    if (d->cols > kJoinMaxCols) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: %lld columns, at most %lld", name, (long long)d->cols, (long long)kJoinMaxCols);
+    if (!join_extents_ok(d)) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: %lld rows of %lld columns, at most 2^60 elements in rows of %lld", name, (long long)d->rows, (long long)d->cols, (long long)kJoinMaxCols);
     if (!(d->eps >= 0.0f) || !(d->p >= 0.0f && d->p <= 1.0f) || std::isinf(d->eps)) return fail(QBP_ERR_INVALID_ARG, "%s: eps %g, p %g", name, (double)d->eps, (double)d->p);
     if (d->index_base % 8) return fail(QBP_ERR_INVALID_ARG, "%s: index_base %llu is not a multiple of 8", name, (unsigned long long)d->index_base);
     if (!b && d->rows > 0 && d->cols > 0 && (d->post || gate || d->p > 0.0f)) return fail(QBP_ERR_INVALID_ARG, "%s: a norm after, a gate or dropout without a block output", name);
@@ -383,7 +388,8 @@ static inline int join_empty(void *ws, size_t ws_bytes, cudaStream_t st)
     return QBP_OK;
 }
 static inline bool real_ok(const void *p, int dtype) { return p && aligned_to(p, dtype_size(dtype)); }
-static inline int64_t join_gates(const qbp_resnorm_desc *d) { return d->gate_rows ? (d->rows + d->gate_rows - 1) / d->gate_rows : 1; }
+// Rows that share a row of the gate: of those that there are, however many more a gate row is for.
+static inline int64_t join_gate_rows(const qbp_resnorm_desc *d) { return std::max<int64_t>(d->gate_rows ? std::min(d->gate_rows, d->rows) : d->rows, 1); }
 
 // How the rows are cut for a grid of at most `most` blocks: items of neighbouring rows of one gate.
 struct JoinCut { JoinItems it; int64_t blocks; };
@@ -392,8 +398,8 @@ static inline JoinCut join_cut(const qbp_resnorm_desc *d, const JoinShape &s, bo
     JoinCut c{};
     JoinItems &it = c.it;
     it.rows = d->rows; it.cols = d->cols;
-    it.gates = per_gate && d->gate_rows ? join_gates(d) : 1;
-    it.gate_rows = per_gate && d->gate_rows ? d->gate_rows : std::max<int64_t>(d->rows, 1);
+    it.gate_rows = per_gate ? join_gate_rows(d) : std::max<int64_t>(d->rows, 1);
+    it.gates = std::max<int64_t>((d->rows + it.gate_rows - 1) / it.gate_rows, 1);
     if (s.warp) few *= kJoinWarpRows;                                // a block takes so many rows at a time
     it.splits = std::max<int64_t>(1, std::min((most + it.gates - 1) / it.gates, (it.gate_rows + few - 1) / few));
     it.split_rows = (it.gate_rows + it.splits - 1) / it.splits;

@@ -396,7 +396,7 @@ static JoinCut join_cut_bwd(const qbp_resnorm_desc *d, bool per_gate)
 
 extern "C" __attribute__((visibility("default"))) size_t qbp_resnorm_bwd_workspace_bytes(const qbp_resnorm_desc *d)
 {
-    if (!d || d->rows <= 0 || d->cols <= 0) return 256;
+    if (!d || !join_extents_ok(d) || d->rows == 0 || d->cols == 0) return 256;
     size_t most = 0;
     for (bool per_gate : {false, true}) {
         const JoinCut c = join_cut_bwd(d, per_gate);
