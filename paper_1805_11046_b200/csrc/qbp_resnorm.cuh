@@ -199,7 +199,8 @@ template <bool VEC> __host__ __device__ constexpr uint32_t join_section(uint32_t
 // How far behind its section's start a row begins.
 __device__ __forceinline__ uint32_t join_shift(const JoinSource &s, int64_t row) { return ((uint32_t)reinterpret_cast<uintptr_t>(s.row0) + (uint32_t)row * s.row_bytes) & 15u; }
 // A row off the 16-byte boundaries, by one lane: the 16-byte pieces that lie within the tensor as one copy, the others, which hold the
-// tensor's first or last elements, by hand.
+// tensor's first or last elements, by hand (and fenced: the slot's next row is copied over them by the asynchronous proxy, ahead of which
+// barriers alone order no ordinary store).
 template <typename T> __device__ __forceinline__ void join_copy_from_before(uint8_t *section, uint64_t *full, const JoinSource &s, int64_t row, int64_t rows)
 {
     const uintptr_t first = reinterpret_cast<uintptr_t>(s.row0), a = first + (uintptr_t)(row * s.row_bytes), e = a + s.row_bytes, base = a & ~(uintptr_t)15;
@@ -208,6 +209,7 @@ template <typename T> __device__ __forceinline__ void join_copy_from_before(uint
         lo = max(lo, (first + 15) & ~(uintptr_t)15); hi = min(hi, (first + (uintptr_t)(rows * s.row_bytes)) & ~(uintptr_t)15);
         for (uintptr_t p = a; p < min(e, lo); p += sizeof(T)) *reinterpret_cast<T *>(section + (p - base)) = *reinterpret_cast<const T *>(p);
         for (uintptr_t p = max(a, hi); p < e; p += sizeof(T)) *reinterpret_cast<T *>(section + (p - base)) = *reinterpret_cast<const T *>(p);
+        fence_proxy_async();
         if (lo >= hi) return;
     }
     mbar_expect_bytes(full, (uint32_t)(hi - lo));
