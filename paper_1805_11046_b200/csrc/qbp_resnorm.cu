@@ -90,14 +90,16 @@ join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ Ph
                     if (P.b) {
                         float b[8];
                         ring_read<TB, VEC>(my_b, c0 + k * apart, in[k], b);
-                        if (P.drop) {                 // (what is dropped counts for nothing, whatever it is: chosen, not multiplied by zero)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) b[e] *= scale;
+                        if (P.drop) {                 // (what is dropped counts for nothing, whatever it or its row's norm is: chosen, not multiplied by zero)
                             Kept<VEC> kept;
                             kept.make(P.d, keys, P.drop, row * cols, 256 * warp + k * apart);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) b[e] = kept[e] ? b[e] : 0.0f;
                         }
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) r[k][e] = fmaf(b[e] * scale, gw[k][e], r[k][e]);
+                        for (int e = 0; e < 8; ++e) r[k][e] = fmaf(b[e], gw[k][e], r[k][e]);
                     }
                     join_put<TX, VEC>(P.r, at + k * apart, in[k], P.wide, r[k]);
 #pragma unroll
