@@ -132,13 +132,17 @@ join_bwd_kernel(const __grid_constant__ JoinBwdParams P, const __grid_constant__
                         g[e] = fmaf(h[e], rstd2, g[e]);
                         if (kHold) V[e] = g[e];
                     }
-                    if (P.drop) {
+                    if (P.drop) {                     // (what is dropped has no part in the sums, whatever its gradient is: chosen, not multiplied by zero)
                         Kept<VEC> q;
                         q.make(P.d, keys, P.drop, at - (VEC ? 8 : 1) * lane + k * apart, 0);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) { const bool on = q[e]; kept |= on ? 1u << (8 * k + e) : 0u; b[e] = on ? b[e] : 0.0f; }
-                    }
-                    if (P.post) {
+                        for (int e = 0; e < 8; ++e)
+                            if (q[e]) {               // (the sums: of use with a norm after the block alone)
+                                kept |= 1u << (8 * k + e);
+                                sums[1] = fmaf(g[e], b[e], sums[1]);
+                                sums[2] = fmaf(r[e], b[e], sums[2]);
+                            }
+                    } else if (P.post) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             sums[1] = fmaf(g[e], b[e], sums[1]);

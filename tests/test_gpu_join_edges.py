@@ -65,3 +65,28 @@ def test_what_is_dropped_of_a_row_without_a_norm(B, rows, cols, stream):
     _, _, e1, eg, _ = B.qbp_resnorm_bwd(d, dr2, None, b2, r, q1.clone().index_fill_(0, torch.tensor([1, 2, 3], device="cuda"), 1.0), None, i["w1"], i["gate"])
     gone = ~k[1:4].any(0)
     assert torch.equal(dw1[gone], e1[gone]) and torch.equal(dg[0][gone], eg[0][gone])
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("types", [("float32", "float32"), ("bfloat16", "bfloat16")])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_gradient_that_is_not_finite(B, rows, cols, types, bad):
+    """One element of dr: its own dx, its row's db and its column's dgate and dw_post, none of these but dx where the element was dropped."""
+    import torch
+    i = {k: v[0] for k, v in inputs(rows, cols, *types, 1, 23).items()}
+    k = F.keep((rows, cols), 0.5, 12, 3) != 0
+    kw = dict(p=0.5, seed=12, tensor_id=3)
+    want = both_passes(B, i, **kw)
+    at = {on: next((a, c) for a in range(rows - 1, -1, -1) for c in range(cols - 1, -1, -1) if k[a, c] == on) for on in (True, False)}
+    for on, (a, c) in at.items():
+        dr = i["dr"].clone()
+        dr[a, c] = bad
+        got = both_passes(B, {**i, "dr": dr}, **kw)
+        spoilt = [torch.zeros_like(t, dtype=torch.bool) for t in want]
+        spoilt[4][a, c] = True                                   # dx
+        if on:
+            spoilt[5][a] = True                                  # db
+            spoilt[6][c] = True; spoilt[7][0, c] = True          # dw_post, dgate
+        for n, (g, w, s) in enumerate(zip(got, want, spoilt)):
+            assert torch.equal(~torch.isfinite(g), s), (n, on)
+            assert torch.equal(g[~s], w[~s]), (n, on)
