@@ -10,6 +10,7 @@ message.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import threading
 from pathlib import Path
 
@@ -497,7 +498,7 @@ def _rows_of(x):
     if not x.is_contiguous():
         raise ValueError("a tensor of other than two dimensions has to be contiguous")
     cols = x.shape[-1] if x.dim() else 1
-    return (x.numel() // cols if cols else 0), cols, cols
+    return x.numel() // cols if cols else math.prod(x.shape[:-1]), cols, cols           # (rows without columns are rows too)
 
 
 def _addr(t):
