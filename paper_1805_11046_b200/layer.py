@@ -4,6 +4,8 @@ gradient copies, workspace) as torch tensors and passes their addresses
 through the C ABI.  No arithmetic happens here."""
 from __future__ import annotations
 
+import threading
+
 import torch
 
 from . import binding as B
@@ -191,14 +193,16 @@ class _F8Space:
     add up to no more than the newest)."""
 
     def __init__(self, words, device):
-        self.words, self.device, self.kept = words, device, []
+        self.words, self.device, self.kept = words, torch.device(device), []
 
     def get(self, scratch=0):
         """The workspace, with at least so many bytes behind its words."""
         need = 256 * self.words + scratch
         if not self.kept or self.kept[-1].numel() < need:
             size = max(need, 2 * self.kept[-1].numel() if self.kept else 0)
-            self.kept.append(torch.zeros(-(-size // 256) * 256, dtype=torch.uint8, device=self.device))
+            # (one that is first asked for within a capture is not cleared: the graph would clear it in every replay, other calls' words too)
+            captured = self.device.type == "cuda" and torch.cuda.is_current_stream_capturing()
+            self.kept.append((torch.empty if captured else torch.zeros)(-(-size // 256) * 256, dtype=torch.uint8, device=self.device))
         return self.kept[-1]
 
     def at(self, word, scratch=0):
@@ -207,21 +211,25 @@ class _F8Space:
         return self.get(scratch)[256 * word:]
 
     def status(self) -> int:
-        """0, or the status of a call that failed (synchronises the current stream)."""
-        return min(int(t[:256 * self.words].view(torch.int32)[::64].min()) for t in self.kept) if self.kept else 0
+        """0, or the status of a call that failed (synchronises the current stream).  The kernels raise one status alone; anything else is
+        what a captured call that has not been replayed found in its memory."""
+        failed = any(bool((t[:256 * self.words].view(torch.int32)[::64] == B.QBP_ERR_TIMEOUT).any()) for t in self.kept)
+        return B.QBP_ERR_TIMEOUT if failed else 0
 
 
 class F8Linear:
     """A linear layer y = x w^T in 8-bit floating point with a scale for each block of 128: the activation and the gradient are
     quantised along their rows for y and dx and along their columns for dw, the fp32 master weights w [out_features,
     in_features] in 128 x 128 blocks, once per forward.  Call order and buffers only.  grad_format: B.QBP_E5M2 gives the gradient
-    the wider range.  A layer's calls follow one another (its workspace, codes and saved tensors are its own); in a captured graph
-    they keep their addresses: the codes are written again in place, so that a captured serve() answers with the weights as the last
-    quantise() or forward() found them."""
+    the wider range.  A layer's training calls follow one another (their workspace, the codes, saved tensors and dw are its own, and the next
+    step's calls write them again); serve() may be called from several streams and host threads at a time.  In a captured graph
+    the calls keep their addresses: the codes are written again in place, so that a captured serve()
+    answers with the weights as the last quantise() or forward() found them."""
 
     def __init__(self, w, grad_format=B.QBP_E4M3):
         self.w, self.grad_format = w, grad_format
-        self.space = _F8Space(4, w.device)                                      # dw, dx, y, serve
+        self.space = _F8Space(3, w.device)                                      # dw, dx, y
+        self.serving = {}                                                       # serve()'s, by (stream, host thread)
         self.codes = self.saved = self.dw = None
 
     def quantise(self):
@@ -229,10 +237,18 @@ class F8Linear:
         self.codes = B.qbp_quantize_f8_square(self.w, out=self.codes)
         return self.codes
 
-    def serve(self, x):
-        """y for an activation of any number of rows, from the codes that quantise() or forward() left."""
+    def serve(self, x, ws=None):
+        """y for an activation of any number of rows, from the codes that quantise() or forward() left, outside of a capture for one (a stream
+        that serves has to wait for the one that made them).  The workspace is the stream's and the host thread's own, kept with the layer; a captured graph
+        whose replays may overlap other calls on the stream it was captured on takes a `ws` (qbp_linear_f8_workspace_bytes,
+        its first four bytes the status word)."""
         q, s, _ = self.codes or self.quantise()
-        return B.qbp_linear_f8(x, q, s, ws=self.space.at(3, B.qbp_linear_f8_workspace_bytes(x.numel() // max(x.shape[-1], 1), *q.shape)))
+        if ws is None:
+            key = B._stream_handle(self.w.get_device()), threading.get_ident()
+            space = self.serving.get(key)
+            if space is None: space = self.serving[key] = _F8Space(1, self.w.device)
+            ws = space.get(B.qbp_linear_f8_workspace_bytes(x.numel() // max(x.shape[-1], 1), *q.shape) - 256)
+        return B.qbp_linear_f8(x, q, s, ws=ws)
 
     def forward(self, x):
         q, s, _ = self.quantise()
@@ -250,7 +266,8 @@ class F8Linear:
         return dx
 
     def status(self) -> int:
-        return self.space.status()
+        """The worst status of the layer's calls that the current stream has waited for, on whichever streams they were."""
+        return min(space.status() for space in [self.space, *self.serving.values()])
 
 
 class F8ResidualStack:

@@ -14,3 +14,38 @@ def test_rows_without_columns_are_rows(B):
     import torch
     for shape, rows in (((3, 0), 3), ((2, 3, 0), 6), ((2, 0, 0), 0), ((0,), 1), ((4, 0, 16), 0), ((2, 3, 16), 6)):
         assert B._rows_of(torch.empty(shape)) == (rows, shape[-1], shape[-1])
+
+
+def test_serving_from_several_streams_and_threads_shares_no_scratch(B, monkeypatch):
+    """Calls that may run at the same time quantise their activations into workspaces of their own; those of one stream and thread keep theirs."""
+    import threading
+
+    import torch
+    from paper_1805_11046_b200 import layer
+    now, used = {"stream": 7}, []
+    monkeypatch.setattr(B, "_stream_handle", lambda device: now["stream"])
+    monkeypatch.setattr(B, "qbp_linear_f8", lambda x, q, s, ws: used.append((ws.data_ptr(), ws.numel(), ws)))
+    L = layer.F8Linear(torch.zeros(32, 64))
+    L.codes = torch.zeros(32, 64, dtype=torch.uint8), None, None
+    x, more = torch.zeros(100, 64), torch.zeros(4000, 64)
+    L.serve(x)
+    now["stream"] = 9
+    L.serve(x)
+    t = threading.Thread(target=lambda: L.serve(x))
+    t.start(); t.join()
+    spans = sorted((a, a + n) for a, n, _ in used)
+    assert all(end <= start for (_, end), (start, _) in zip(spans, spans[1:]))
+    assert all(n >= B.qbp_linear_f8_workspace_bytes(100, 32, 64) for _, n, _ in used)
+    L.serve(x)
+    assert used[-1][0] == used[1][0]                        # this stream's again
+    L.serve(more)
+    assert used[-1][1] >= B.qbp_linear_f8_workspace_bytes(4000, 32, 64)
+    own = torch.zeros(1 << 20, dtype=torch.uint8)
+    L.serve(x, ws=own)
+    assert used[-1][2] is own
+    # a failed call of any of them is not forgotten, nor one of a training step's
+    for ws in (used[0][2], used[2][2], L.space.at(1)):
+        assert L.status() == 0
+        ws[:4].view(torch.int32)[0] = -6
+        assert L.status() == -6
+        ws[:4] = 0
