@@ -460,7 +460,8 @@ def _dtype(t) -> int:
         raise TypeError(f"{t}: fp32, bf16 or fp16 is wanted") from None
 
 
-_current_device = torch._C._cuda_getDevice          # (torch.cuda.current_device() without its check for a first use, which every tensor has had)
+# (torch.cuda.current_device() without its check for a first use, which every tensor has had; a torch without CUDA has neither of the two)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _EMPTY = {}
 
 

@@ -49,3 +49,17 @@ def test_serving_from_several_streams_and_threads_shares_no_scratch(B, monkeypat
         ws[:4].view(torch.int32)[0] = -6
         assert L.status() == -6
         ws[:4] = 0
+
+
+def test_the_binding_imports_on_a_torch_without_cuda(B):
+    """Such a torch has no raw lookups of the current device and stream; the module's own are looked up with something to fall back on."""
+    import subprocess
+    import sys
+    from pathlib import Path
+    code = ("import torch\n"
+            "for name in ('_cuda_getDevice', '_cuda_getCurrentRawStream'):\n"
+            "    if hasattr(torch._C, name): delattr(torch._C, name)\n"
+            "from paper_1805_11046_b200 import binding, layer\n"
+            "assert binding._current_device is torch.cuda.current_device and binding._raw_stream is None\n")
+    got = subprocess.run([sys.executable, "-c", code], cwd=Path(__file__).resolve().parent.parent, capture_output=True, text=True)
+    assert got.returncode == 0, got.stderr
