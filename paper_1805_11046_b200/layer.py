@@ -277,7 +277,9 @@ class F8ResidualStack:
     repeats its draws of the dropout: their number is an argument of its calls."""
 
     def __init__(self, weights, alpha=1.0, eps=1e-6, p=0.0, seed=0, lr=0.1, momentum=0.9, weight_decay=0.0, grad_format=B.QBP_E5M2):
-        """weights: [C, C] fp32 device tensors, one for each block, updated in place."""
+        """weights: [C, C] fp32 device tensors, one for each block, updated in place, and so no two of them in the same memory."""
+        spans = sorted((w.data_ptr(), w.data_ptr() + w.numel() * w.element_size()) for w in weights)
+        if any(end > start for (_, end), (start, _) in zip(spans, spans[1:])): raise ValueError("two blocks' weights share memory: each would be updated by both gradients at once")
         self.linears = [F8Linear(w, grad_format) for w in weights]
         C, dev = weights[0].shape[0], weights[0].device
         ones = lambda: torch.ones(C, dtype=torch.float32, device=dev)

@@ -63,3 +63,16 @@ def test_the_binding_imports_on_a_torch_without_cuda(B):
             "assert binding._current_device is torch.cuda.current_device and binding._raw_stream is None\n")
     got = subprocess.run([sys.executable, "-c", code], cwd=Path(__file__).resolve().parent.parent, capture_output=True, text=True)
     assert got.returncode == 0, got.stderr
+
+
+def test_blocks_that_share_weights_are_refused(B):
+    """Their update would be two writers of the same memory."""
+    import torch
+    from paper_1805_11046_b200 import layer
+    w = [torch.zeros(16, 16) for _ in range(3)]
+    assert len(layer.F8ResidualStack(w).linears) == 3
+    both = torch.zeros(31, 16)
+    for weights in ([w[0], w[1], w[0]], [both[:16], both[15:]]):
+        with pytest.raises(ValueError, match="share memory"):
+            layer.F8ResidualStack(weights)
+    assert len(layer.F8ResidualStack([both[:15], both[15:30]]).linears) == 2
