@@ -628,7 +628,8 @@ int qbp_gated_xnor_gemm_bits(int64_t M, int64_t N, int64_t K, const uint32_t *nz
  *
  * Real-valued tensors are fp32, bf16 or fp16 (qbp_dtype); all arithmetic is
  * fp32, and a result is rounded once, as it is stored.  Every tensor is on
- * the stream's device.
+ * the stream's device.  The rows of a tensor that is quantised and of an output are
+ * at most 128 * 65535, other extents 2^30 (more: QBP_ERR_UNSUPPORTED_SHAPE).
  * ---------------------------------------------------------------------- */
 typedef enum { QBP_F32 = 0, QBP_BF16 = 1, QBP_F16 = 2 } qbp_dtype;
 enum { QBP_E4M3 = 0, QBP_E5M2 = 1 };

@@ -593,7 +593,7 @@ static int launch_f8_split(const F8Product &p, const SplitInput &in, cudaStream_
 
 // ================================================================= entry points
 constexpr int64_t kF8MaxExtent = (int64_t)1 << 30;                  // TMA coordinates and the grid are 32-bit
-constexpr int64_t kF8MaxRowTiles = 65535;
+constexpr int64_t kF8MaxRows = 65535 * 128;                         // the grid's second extent
 
 static int check_quantize(const char *name, const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int format)
 {
@@ -601,7 +601,7 @@ static int check_quantize(const char *name, const void *x, int dtype, int64_t ro
     if (format != QBP_E4M3 && format != QBP_E5M2) return fail(QBP_ERR_INVALID_ARG, "%s: format %d", name, format);
     if (rows < 0 || cols < 0 || ld < cols) return fail(QBP_ERR_INVALID_ARG, "%s: rows %lld, cols %lld, ld %lld", name, (long long)rows, (long long)cols, (long long)ld);
     if (cols % 16) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: cols %lld is not a multiple of 16", name, (long long)cols);
-    if (f8_blocks(rows) > kF8MaxRowTiles || cols > kF8MaxExtent) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: %lld x %lld", name, (long long)rows, (long long)cols);
+    if (rows > kF8MaxRows || cols > kF8MaxExtent) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: %lld x %lld", name, (long long)rows, (long long)cols);
     if (rows == 0 || cols == 0) return QBP_OK;
     if (!x || !aligned_to(x, dtype_size(dtype))) return fail(QBP_ERR_INVALID_ARG, "%s: x is NULL or misaligned", name);
     return QBP_OK;
@@ -653,7 +653,7 @@ static int check_product(const F8Product &p, const char *name)
     const int64_t inner_a = p.transA ? p.M : p.K, inner_b = p.transB ? p.K : p.N;
     if (inner_a % 16 || inner_b % 16)
         return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: the operands' innermost extents %lld and %lld are not multiples of 16", name, (long long)inner_a, (long long)inner_b);
-    if (p.M > kF8MaxExtent || p.N > kF8MaxExtent || p.K > kF8MaxExtent || (p.M + 127) / 128 > kF8MaxRowTiles)
+    if (p.M > kF8MaxExtent || p.N > kF8MaxExtent || p.K > kF8MaxExtent || p.M > kF8MaxRows)
         return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: %lld x %lld x %lld", name, (long long)p.M, (long long)p.N, (long long)p.K);
     return QBP_OK;
 }

@@ -76,3 +76,17 @@ def test_blocks_that_share_weights_are_refused(B):
         with pytest.raises(ValueError, match="share memory"):
             layer.F8ResidualStack(weights)
     assert len(layer.F8ResidualStack([both[:15], both[15:30]]).linears) == 2
+
+
+def test_extents_that_the_grids_cannot_have(B):
+    """Refused on the host, up to the ends of 64 bits; the largest ones pass these checks and fail a later one here."""
+    P, most = 4096, (1 << 63) - 1
+    rows, wide = 128 * 65535, 1 << 30
+    for r, c in ((rows + 1, 16), (most, 16), (most - 126, 32), (1 << 40, 16), (1, wide + 16), (16, most - 15)):
+        assert B.lib.qbp_quantize_f8(P, 0, r, c, c, 0, P, P, P, P, None) == -2, (r, c)
+        assert B.lib.qbp_quantize_f8_square(P, 0, r, c, c, 0, P, P, P, None) == -2, (r, c)
+        assert B.lib.qbp_linear_f8(P, 0, c, r, 16, c, 0, P, P, P, P, most, None) == -2, (r, c)
+    assert B.lib.qbp_quantize_f8(P, 0, rows, wide, wide, 0, None, None, None, None, None) == -1      # (no output)
+    for M, N, K in ((rows + 1, 16, 16), (most, 16, 16), (16, wide + 1, 16), (16, most, 16), (16, 16, wide + 16), (16, 16, most - 15)):
+        assert B.lib.qbp_gemm_f8(0, 1, M, N, K, 0, P, P, 0, P, P, 0, P, P, most, None) == -2, (M, N, K)
+    assert B.lib.qbp_gemm_f8(0, 1, rows, wide, wide, 0, P, P, 0, P, P, 0, None, P, most, None) == -1
