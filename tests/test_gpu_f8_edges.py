@@ -84,3 +84,46 @@ def test_graphs_of_one_layer_replay_at_the_same_time(B):
     assert all(B.status_word(ws) == 0 for ws in wss)
     g.replay()
     assert torch.equal(y, want[0]) and L.status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("bad", [np.nan, -np.nan, np.inf, -np.inf])
+def test_blocks_that_are_not_finite_in_every_type_and_direction(B, dtype, bad):
+    """One such element in a first, a middle and a ragged last block: NaN codes and scales there, all other codes and scales as ever; products
+    and layers of few and of many rows answer NaN where these blocks enter and nowhere else."""
+    import torch
+    rows, cols, N = 300, 400, 48
+    v = rng(6).standard_normal((rows, cols)).astype(np.float32)
+    at = [(0, 0), (130, 200), (299, 399)]
+    x = torch.from_numpy(v).to(getattr(torch, dtype)).cuda()
+    for i, j in at: x[i, j] = bad
+    d = x.double().cpu().numpy()
+    qr, sr, qc, sc = B.qbp_quantize_f8(x, cols=True)
+    for q, s, got in ((*F.quantize(d, 0, 1, 128), (qr, sr)), (*[t for t in F.quantize(d, 0, 128, 1)], (qc, sc))):
+        across = got[0] is qc
+        assert np.array_equal(host(got[0]), q) and np.array_equal(host(got[1]), F.pack(s.T if across else s, cols if across else rows))
+        assert (s == 128).sum() == 3
+    q, s1, s2 = B.qbp_quantize_f8_square(x)
+    wq, we = F.quantize(d, 0, 128, 128)
+    assert (we == 128).sum() == 3 and np.array_equal(host(q), wq)
+    assert np.array_equal(host(s1), F.pack(F.spread(we, rows, 0), rows)) and np.array_equal(host(s2), F.pack(F.spread(we.T, cols, 0), cols))
+    w, sw, _ = B.qbp_quantize_f8_square(torch.from_numpy(rng(7).standard_normal((N, cols)).astype(np.float32)).cuda())
+    want = np.zeros((rows, N), bool)
+    want[[i for i, _ in at]] = True
+    for some in (slice(0, 300), slice(128, 133), slice(299, 300), slice(290, 300)):
+        y = B.qbp_linear_f8(x[some], w, sw)
+        assert np.array_equal(np.isnan(host(y.float())), want[some]) and bool(torch.isfinite(y[~torch.isnan(y)]).all())
+    # as weights, one scale for 128 x 128: the columns of the outputs whose blocks hold one of them
+    z = B.qbp_gemm_f8(w, sw, q, s1, transB=True)
+    assert np.array_equal(np.isnan(host(z)).all(0), F.spread((we == 128).any(1)[None], rows)[0]) and np.array_equal(np.isnan(host(z)).any(0), np.isnan(host(z)).all(0))
+
+
+@pytest.mark.parametrize("fmt", [0, 1])
+def test_weights_quantised_into_storage_made_before(B, fmt):
+    """Codes and scales written over storage that qbp_f8_scales sized, whatever it held."""
+    import torch
+    rows, cols = 210, 144
+    x = torch.from_numpy(rng(8).standard_normal((rows, cols)).astype(np.float32)).cuda()
+    out = torch.full((rows, cols), 255, dtype=torch.uint8, device="cuda"), B.qbp_f8_scales(rows, cols).fill_(3), B.qbp_f8_scales(cols, rows).fill_(3)
+    got = B.qbp_quantize_f8_square(x, format=fmt, out=out)
+    assert all(a is b for a, b in zip(got, out)) and all(torch.equal(a, b) for a, b in zip(got, B.qbp_quantize_f8_square(x, format=fmt)))

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import f8_oracle as F
-from tests.test_gpu_resnorm import EPS, check, inputs
+from tests.test_gpu_resnorm import EPS, U, check, close, host, inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -90,3 +90,77 @@ def test_a_gradient_that_is_not_finite(B, rows, cols, types, bad):
         for n, (g, w, s) in enumerate(zip(got, want, spoilt)):
             assert torch.equal(~torch.isfinite(g), s), (n, on)
             assert torch.equal(g[~s], w[~s]), (n, on)
+
+
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_a_block_output_or_gradient_of_h_that_is_not_finite(B, rows, cols):
+    """An infinity in dh or a NaN in b: the rows that hold them and, of the parameters' gradients, every column that such a row enters; no other row."""
+    import torch
+    i = {k: v[0] for k, v in inputs(rows, cols, "float32", "bfloat16", 1, 29).items()}
+    want = both_passes(B, i)
+    dh, b = i["dh"].clone(), i["b"].clone()
+    dh[3, 2] = float("inf"); b[4, cols - 1] = float("nan")
+    r, h, q1, q2, dx, db, dw1, dg, dw2 = both_passes(B, {**i, "dh": dh, "b": b})
+    rest = [j for j in range(rows) if j not in (3, 4)]
+    for got, w in zip((r, h, q1, q2, dx, db), want):
+        assert torch.equal(got[rest], w[rest])
+    assert torch.equal(r[3], want[0][3]) and not torch.isfinite(r[4]).any() and not torch.isfinite(h[4]).any()
+    assert not torch.isfinite(dx[3:5]).any() and not torch.isfinite(db[3:5]).any()
+    assert not torch.isfinite(dw1).any() and not torch.isfinite(dg).any() and not torch.isfinite(dw2).any()      # (row 4's norms are of no number)
+
+
+# ------------------------------------------------------------------------ whole 16-byte pieces from another boundary
+@pytest.mark.parametrize("rows,cols", [(21, 512), (40, 1000), (14, 4096), (9, 8192), (5, 16384)])
+@pytest.mark.parametrize("off", ["x", "b", "w1", "w2", "gate", "dr", "dh"])
+def test_a_tensor_off_the_16_byte_boundary_against_the_definition(B, rows, cols, off, monkeypatch):
+    """One input an element behind a boundary: every output within the bounds of an aligned call."""
+    import torch
+    import tests.test_gpu_resnorm as R
+
+    def moved(*args):
+        i = inputs(*args)
+        t, v = i[off]
+        return {**i, off: (torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")[1:].view(t.shape).copy_(t), v)}
+
+    monkeypatch.setattr(R, "inputs", moved)
+    check(B, rows, cols, "float32", "bfloat16", gate_rows=0, p=0.3, alpha=0.5)
+
+
+@pytest.mark.parametrize("cols", [512, 4096, 16384])
+def test_outputs_off_the_16_byte_boundary(B, cols):
+    """Any one of them: the bits of the call with an input there."""
+    import torch
+    i = {k: v[0] for k, v in inputs(19, cols, "float32", "bfloat16", 1, 31).items()}
+    off = lambda t: torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")[1:].view(t.shape)
+    d = B.resnorm_desc(i["x"], i["b"], p=0.3, seed=4)
+    params = i["w1"], i["gate"], i["w2"]
+    want = B.qbp_resnorm_fwd(d, off(i["x"]).copy_(i["x"]), i["b"], *params)
+    for kw in (dict(r=off(i["x"])), dict(h=off(i["b"]))):
+        assert all(torch.equal(a, c) for a, c in zip(B.qbp_resnorm_fwd(d, i["x"], i["b"], *params, **kw), want))
+    r, _, q1, q2 = want
+    grads = B.qbp_resnorm_bwd(d, off(i["dr"]).copy_(i["dr"]), i["dh"], i["b"], r, q1, q2, *params)
+    for kw in (dict(dx=off(i["x"])), dict(db=off(i["b"]))):
+        assert all(torch.equal(a, c) for a, c in zip(B.qbp_resnorm_bwd(d, i["dr"], i["dh"], i["b"], r, q1, q2, *params, **kw), grads))
+
+
+# ------------------------------------------------------------------------ dropout
+@pytest.mark.parametrize("dtype,n", [("float32", 10_000_003), ("bfloat16", 20_000_003), ("float16", 20_000_005)])
+@pytest.mark.parametrize("off", [0, 16, 0.5])
+def test_long_dropout_is_that_of_its_pieces(B, dtype, n, off):
+    """More elements than the device's threads take one block of eight each of: every element is that of a call on a short piece; from a 32-byte
+    boundary, from a 16-byte one (off: bytes; 0.5: one element) and from neither, with a ragged end."""
+    import torch
+    t = getattr(torch, dtype)
+    first = int(off / t.itemsize) if off > 1 else int(off > 0)
+    x = torch.randn(n + 16, device="cuda", generator=torch.Generator("cuda").manual_seed(n)).to(t)[first:first + n]
+    assert x.data_ptr() % 32 == int(off if off != 0.5 else t.itemsize)
+    y = torch.empty(n + 16, dtype=t, device="cuda")[first:first + n]
+    base = (1 << 33) + 40
+    B.qbp_dropout(x, 0.3, 99, tensor_id=2, index_base=base, y=y)
+    step = 1 << 20
+    for at in range(0, n, step):
+        assert torch.equal(y[at:at + step], B.qbp_dropout(x[at:at + step], 0.3, 99, tensor_id=2, index_base=base + at)), at
+    for at in (0, n // 2 // 8 * 8, n - n % 8 - 4096):
+        piece = slice(at, min(at + 5000, n))
+        k = F.keep((piece.stop - at,), 0.3, 99, 2, base + at)
+        close(y[piece], host(x[piece]) * k, 2 * U * np.abs(host(x[piece]) * k), dtype)
