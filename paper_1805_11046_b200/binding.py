@@ -550,7 +550,8 @@ def qbp_quantize_f8(x, format=QBP_E4M3, rows=True, cols=False):
 
 def qbp_quantize_f8_square(x, format=QBP_E4M3, out=None):
     """Codes of x [rows, columns] with one scale for each 128 x 128 block, and the scales for products that reduce over the
-    columns and over the rows: (q, s_rows, s_cols).  out: an earlier call's three tensors, to be written again."""
+    columns and over the rows: (q, s_rows, s_cols).  out: three such tensors to be written (an earlier call's, or codes like x and two
+    tensors of qbp_f8_scales)."""
     device = _here(x, *(out or ()))
     r, c, ld = _rows_of(x)
     if out is None:

@@ -91,9 +91,8 @@ template <int FORMAT> __device__ __forceinline__ uint2 f8_codes8(const float (&v
     return make_uint2(f8_codes4<FORMAT>(v[0], v[1], v[2], v[3]), f8_codes4<FORMAT>(v[4], v[5], v[6], v[7]));
 }
 
-// Largest magnitudes of eight elements and more, as they are held: of the halves two to a word.  A NaN is passed on.
+// The larger of two magnitudes, of the halves two to a word as they are held.  A NaN is passed on.
 template <typename T> struct HalfMax {
-    uint32_t m[4] = {0, 0, 0, 0};
     static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
     {
         uint32_t r;
