@@ -236,7 +236,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_fwd(const qbp_
     if (!ws || !aligned_to(ws, 256) || ws_bytes < 256) return fail(QBP_ERR_WORKSPACE, "resnorm_fwd: workspace NULL, misaligned or smaller than 256 bytes");
     JoinParams P{};
     const bool vec = d->cols % 8 == 0 && aligned16(x) && aligned16(b) && aligned16(r) && aligned16(h) && aligned16(w_post) && aligned16(gate) && aligned16(w_pre);
-    const JoinShape s = join_shape(d, 1);
+    const JoinShape s = join_shape(d, 1, vec);
     const JoinCut c = join_cut(d, s, gate != nullptr, join_blocks(d, s, 1), 1);
     P.it = c.it;
     P.x = x; P.b = b; P.w_post = w_post; P.gate = gate; P.w_pre = w_pre; P.r = r; P.h = h; P.rstd_post = rstd_post; P.rstd_pre = rstd_pre;

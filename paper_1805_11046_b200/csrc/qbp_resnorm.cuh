@@ -317,11 +317,13 @@ constexpr int kJoinWide = 4;                         // times eight columns a th
 #endif
 
 // ================================================================= host side
-struct JoinShape { int ch, threads; bool warp; };
+struct JoinShape { int ch, threads; bool warp, vec; };
 constexpr size_t kJoinMaxRing = 200 * 1024;         // of a block
+// Bytes of a slot for each row that a block takes at once, as the kernel lays it out.
 static inline size_t join_slot(const qbp_resnorm_desc *d, const JoinShape &s, int tensors)
 {
-    return (size_t)(s.warp ? kJoinWarpRows : 1) * (size_t)tensors * (join_section<false>((uint32_t)(d->cols * dtype_size(d->x_dtype))) + join_section<false>((uint32_t)(d->cols * dtype_size(d->b_dtype))));
+    const uint32_t x = (uint32_t)(d->cols * dtype_size(d->x_dtype)), b = (uint32_t)(d->cols * dtype_size(d->b_dtype));
+    return (size_t)(s.warp ? kJoinWarpRows : 1) * (size_t)tensors * (s.vec ? join_section<true>(x) + join_section<true>(b) : join_section<false>(x) + join_section<false>(b));
 }
 // Blocks that an SM has threads for (16 warps, which their registers allow; 8 backwards where a row is a warp's).
 static inline int join_per_sm(const JoinShape &s, int tensors) { return s.ch > 2 ? 1 : std::max((s.warp && tensors == 2 ? 256 : 512) / s.threads, 1); }
@@ -337,13 +339,13 @@ static inline size_t join_ring(const qbp_resnorm_desc *d, const JoinShape &s, in
 // Forward a thread takes sixteen columns.  Backwards it takes eight up to 4096 columns: a row's values then stay in registers behind the
 // exchange of its sums, and its slot is free at once (16384 x 4096 232 us, with sixteen 247; 2000 x 2048 bf16 28 and 37).  32 (without a ring)
 // beyond 8192.
-static inline JoinShape join_shape(const qbp_resnorm_desc *d, int tensors)
+static inline JoinShape join_shape(const qbp_resnorm_desc *d, int tensors, bool vec)
 {
     const int chunks = (int)((d->cols + 255) / 256);                 // a warp's eight columns a lane
-    if (chunks <= 2) return {chunks, 32 * kJoinWarpRows, true};
-    const JoinShape s = tensors == 2 && chunks <= 16 ? JoinShape{1, 32 * chunks, false} : JoinShape{2, 32 * ((chunks + 1) / 2), false};
+    if (chunks <= 2) return {chunks, 32 * kJoinWarpRows, true, vec};
+    const JoinShape s = tensors == 2 && chunks <= 16 ? JoinShape{1, 32 * chunks, false, vec} : JoinShape{2, 32 * ((chunks + 1) / 2), false, vec};
     if (s.threads <= 512 && join_ring(d, s, tensors) <= kJoinMaxRing) return s;
-    return {4, 32 * ((chunks + 3) / 4), false};
+    return {4, 32 * ((chunks + 3) / 4), false, vec};
 }
 
 // Runs `call` with the kernel's compile-time choices.

@@ -392,9 +392,8 @@ __global__ void __launch_bounds__(32 * kSumHigh) join_sum_kernel(const __grid_co
 // ================================================================= host side
 // Partial rows of dgate: none where an item is all of a gate's rows, whose sum is the gradient.
 static size_t gate_parts(const JoinItems &it) { return it.splits > 1 ? (size_t)(it.gates * it.splits * it.cols) : 0; }
-static JoinCut join_cut_bwd(const qbp_resnorm_desc *d, bool per_gate)
+static JoinCut join_cut_bwd(const qbp_resnorm_desc *d, const JoinShape &s, bool per_gate)
 {
-    const JoinShape s = join_shape(d, 2);
     return join_cut(d, s, per_gate, join_blocks(d, s, 2), s.warp ? 2 : 4);
 }
 
@@ -402,10 +401,11 @@ extern "C" __attribute__((visibility("default"))) size_t qbp_resnorm_bwd_workspa
 {
     if (!d || !join_extents_ok(d) || d->rows == 0 || d->cols == 0) return 256;
     size_t most = 0;
-    for (bool per_gate : {false, true}) {
-        const JoinCut c = join_cut_bwd(d, per_gate);
-        most = std::max(most, 2 * align_up((size_t)(c.blocks * d->cols) * 4, 256) + align_up(gate_parts(c.it) * 4, 256));
-    }
+    for (bool vec : {false, true})
+        for (bool per_gate : {false, true}) {
+            const JoinCut c = join_cut_bwd(d, join_shape(d, 2, vec), per_gate);
+            most = std::max(most, 2 * align_up((size_t)(c.blocks * d->cols) * 4, 256) + align_up(gate_parts(c.it) * 4, 256));
+        }
     return 256 + most;
 }
 
@@ -437,8 +437,8 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_bwd(const qbp_
         return fail(QBP_ERR_WORKSPACE, "resnorm_bwd: workspace NULL, misaligned or smaller than %zu bytes", qbp_resnorm_bwd_workspace_bytes(d));
     const bool vec = d->cols % 8 == 0 && aligned16(dr) && aligned16(dh) && aligned16(b) && aligned16(r) && aligned16(dx) && aligned16(db) && aligned16(w_post) &&
                      aligned16(gate) && aligned16(w_pre);
-    const JoinShape s = join_shape(d, 2);
-    const JoinCut c = join_cut_bwd(d, gate || dgate);
+    const JoinShape s = join_shape(d, 2, vec);
+    const JoinCut c = join_cut_bwd(d, s, gate || dgate);
     WsCarver w(ws, ws_bytes);
     JoinBwdParams P{};
     P.status = w.take<int>(1);

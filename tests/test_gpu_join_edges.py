@@ -164,3 +164,19 @@ def test_long_dropout_is_that_of_its_pieces(B, dtype, n, off):
         piece = slice(at, min(at + 5000, n))
         k = F.keep((piece.stop - at,), 0.3, 99, 2, base + at)
         close(y[piece], host(x[piece]) * k, 2 * U * np.abs(host(x[piece]) * k), dtype)
+
+
+@pytest.mark.parametrize("cols", [6392, 6396, 6397, 6400, 6408])
+@pytest.mark.parametrize("off", [False, True])
+def test_the_widest_fp32_rows_with_a_ring_backwards(B, cols, off, monkeypatch):
+    """The last widths whose ring has room and the first ones beyond, on the 16-byte boundaries and off them."""
+    import torch
+    import tests.test_gpu_resnorm as R
+
+    def moved(*args):
+        i = inputs(*args)
+        t, v = i["dr"]
+        return {**i, "dr": (torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")[1:].view(t.shape).copy_(t), v)} if off else i
+
+    monkeypatch.setattr(R, "inputs", moved)
+    check(B, 330, cols, "float32", "float32", gate_rows=0, p=0.1, alpha=0.5)
