@@ -698,7 +698,7 @@ int qbp_linear_f8(const void *x, int dtype, int64_t ld, int64_t M, int64_t N, in
  * QBP_RESNORM_MAX_COLS, every tensor aligned to its element (16 bytes and cols a multiple of 8:
  * faster).  rstd_post / rstd_pre [rows] (nullable) receive 1 / RMS for the backward pass.
  * r may be x, and h may be b.  Squares are summed in fp32: a row whose sum of squares passes 3.4e38 has
- * a norm of zeros.  ws: 256 bytes, whose first four are the device status word (see
+ * a norm of zeros, and without eps a row needs magnitudes of 1e-16 and more (squares below 1.2e-38 lose bits).  ws: 256 bytes, whose first four are the device status word (see
  * Conventions), of the backward pass as well.
  * ---------------------------------------------------------------------- */
 #define QBP_RESNORM_MAX_COLS 16384

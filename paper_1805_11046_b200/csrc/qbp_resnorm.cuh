@@ -8,7 +8,7 @@
 // is read from memory twice.  A block takes neighbouring rows of one gate (an item) and keeps the parameters of its columns in registers.  Rows
 // come through a ring of two or three in shared memory, copied whole by one thread (cp.async.bulk): a row is on its way while the one before is
 // worked on, and stays out of the threads' registers.  (Copied by the threads that read it, 16 bytes each, a row of 48 KB took 2100 cycles of
-// their time, of 5900.)  16384 x 4096, fp32 stream, bf16 blocks, dropout: forward 142 us, 5.7 TB/s, backward 204 us, 5.9 TB/s.
+// their time, of 5900.)  16384 x 4096, fp32 stream, bf16 blocks, dropout: forward 142 us, 5.7 TB/s, backward 197 us, 6.1 TB/s.
 //
 // Backwards, with gate and w_post constant along an item's columns, dw_post and dgate are multiples of one sum over its rows,
 // S = sum of R dropout'(b rstd_post): dgate = w_post S, dw_post = gate S.  A thread keeps S and dw_pre's sum in registers, a block leaves
@@ -337,8 +337,9 @@ static inline int join_slots(const qbp_resnorm_desc *d, const JoinShape &s, int 
 }
 static inline size_t join_ring(const qbp_resnorm_desc *d, const JoinShape &s, int tensors) { return (size_t)join_slots(d, s, tensors) * join_slot(d, s, tensors); }
 // Forward a thread takes sixteen columns.  Backwards it takes eight up to 4096 columns: a row's values then stay in registers behind the
-// exchange of its sums, and its slot is free at once (16384 x 4096 232 us, with sixteen 247; 2000 x 2048 bf16 28 and 37).  32 (without a ring)
-// beyond 8192.
+// exchange of its sums, and its slot is free at once (as first built 16384 x 4096 206 us, with sixteen 247; 2000 x 2048 bf16 28 and 37).  32
+// (without a ring) beyond 8192 and where two slots find no room: backwards of fp32 alone from 6400 columns on, 8192 x 8192 1260 us (with
+// bf16 blocks 217).
 static inline JoinShape join_shape(const qbp_resnorm_desc *d, int tensors, bool vec)
 {
     const int chunks = (int)((d->cols + 255) / 256);                 // a warp's eight columns a lane
