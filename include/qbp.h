@@ -694,7 +694,7 @@ int qbp_linear_f8(const void *x, int dtype, int64_t ld, int64_t M, int64_t N, in
  * gate row for all, as with rows or more; gates = ceil(rows / gate_rows)).  w_post, w_pre, gate
  * (each nullable: ones) are fp32.  b == NULL (post and p then 0, gate NULL): the norm before a
  * first block, r = alpha * x; r may be NULL then if alpha is 1, and h is made from x.
- * x and r have x_dtype, b and h b_dtype; rows of any number (up to 2^60 elements in all), cols up to
+ * x and r have x_dtype, b and h b_dtype; rows of any number (up to 2^48 elements in all), cols up to
  * QBP_RESNORM_MAX_COLS, every tensor aligned to its element (16 bytes and cols a multiple of 8:
  * faster).  rstd_post / rstd_pre [rows] (nullable) receive 1 / RMS for the backward pass.
  * r may be x, and h may be b.  Squares are summed in fp32: a row whose sum of squares passes 3.4e38 has

@@ -90,13 +90,14 @@ join_fwd_kernel(const __grid_constant__ JoinParams P, const __grid_constant__ Ph
                     if (P.b) {
                         float b[8];
                         ring_read<TB, VEC>(my_b, c0 + k * apart, in[k], b);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) b[e] *= scale;
-                        if (P.drop) {                 // (what is dropped counts for nothing, whatever it or its row's norm is: chosen, not multiplied by zero)
+if (P.drop) {                 // (what is dropped counts for nothing, whatever it or its row's norm is: chosen, not multiplied by zero)
                             Kept<VEC> kept;
                             kept.make(P.d, keys, P.drop, row * cols, 256 * warp + k * apart);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) b[e] = kept[e] ? b[e] : 0.0f;
+                            for (int e = 0; e < 8; ++e) b[e] = kept[e] ? b[e] * scale : 0.0f;
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) b[e] *= scale;
                         }
 #pragma unroll
                         for (int e = 0; e < 8; ++e) r[k][e] = fmaf(b[e], gw[k][e], r[k][e]);
@@ -237,7 +238,7 @@ extern "C" __attribute__((visibility("default"))) int qbp_resnorm_fwd(const qbp_
     JoinParams P{};
     const bool vec = d->cols % 8 == 0 && aligned16(x) && aligned16(b) && aligned16(r) && aligned16(h) && aligned16(w_post) && aligned16(gate) && aligned16(w_pre);
     const JoinShape s = join_shape(d, 1, vec);
-    const JoinCut c = join_cut(d, s, gate != nullptr, join_blocks(d, s, 1), 1);
+    const JoinCut c = join_cut(d, s, gate != nullptr, join_blocks(d, s, 1), 1, false);
     P.it = c.it;
     P.x = x; P.b = b; P.w_post = w_post; P.gate = gate; P.w_pre = w_pre; P.r = r; P.h = h; P.rstd_post = rstd_post; P.rstd_pre = rstd_pre;
     P.eps = d->eps; P.alpha = d->alpha; P.inv_cols = (float)(1.0 / (double)d->cols);

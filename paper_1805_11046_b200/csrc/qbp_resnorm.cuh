@@ -369,17 +369,17 @@ static int launch_join(void (*kernel)(Params, PhiloxKeys), PerDeviceOnce &once, 
     return QBP_OK;
 }
 
-// Whether rows, columns and gate_rows are such that no count made of them overflows (2^60 elements at most).
+// Whether rows, columns and gate_rows are such that no count made of them overflows (2^48 elements at most).
 static inline bool join_extents_ok(const qbp_resnorm_desc *d)
 {
-    return d->rows >= 0 && d->cols >= 0 && d->gate_rows >= 0 && d->cols <= kJoinMaxCols && d->rows <= ((int64_t)1 << 60) / std::max<int64_t>(d->cols, 1);
+    return d->rows >= 0 && d->cols >= 0 && d->gate_rows >= 0 && d->cols <= kJoinMaxCols && d->rows <= ((int64_t)1 << 48) / std::max<int64_t>(d->cols, 1);
 }
 static inline int check_join(const qbp_resnorm_desc *d, const char *name, const void *b, const float *gate, const float *w_post, const float *w_pre)
 {
     if (!d) return fail(QBP_ERR_INVALID_ARG, "%s: NULL descriptor", name);
     if (!dtype_ok(d->x_dtype) || !dtype_ok(d->b_dtype)) return fail(QBP_ERR_INVALID_ARG, "%s: dtypes %d and %d", name, d->x_dtype, d->b_dtype);
     if (d->rows < 0 || d->cols < 0 || d->gate_rows < 0) return fail(QBP_ERR_INVALID_ARG, "%s: rows %lld, cols %lld, gate_rows %lld", name, (long long)d->rows, (long long)d->cols, (long long)d->gate_rows);
-    if (!join_extents_ok(d)) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: %lld rows of %lld columns, at most 2^60 elements in rows of %lld", name, (long long)d->rows, (long long)d->cols, (long long)kJoinMaxCols);
+    if (!join_extents_ok(d)) return fail(QBP_ERR_UNSUPPORTED_SHAPE, "%s: %lld rows of %lld columns, at most 2^48 elements in rows of %lld", name, (long long)d->rows, (long long)d->cols, (long long)kJoinMaxCols);
     if (!(d->eps >= 0.0f) || !(d->p >= 0.0f && d->p <= 1.0f) || std::isinf(d->eps)) return fail(QBP_ERR_INVALID_ARG, "%s: eps %g, p %g", name, (double)d->eps, (double)d->p);
     if (d->index_base % 8) return fail(QBP_ERR_INVALID_ARG, "%s: index_base %llu is not a multiple of 8", name, (unsigned long long)d->index_base);
     if (!b && d->rows > 0 && d->cols > 0 && (d->post || gate || d->p > 0.0f)) return fail(QBP_ERR_INVALID_ARG, "%s: a norm after, a gate or dropout without a block output", name);
@@ -399,11 +399,14 @@ static inline int64_t join_gate_rows(const qbp_resnorm_desc *d) { return std::ma
 
 // How the rows are cut for a grid of at most `most` blocks: items of neighbouring rows of one gate.  Blocks take items in turn, and the time
 // is that of the block with the most: items fill whole rounds of the grid, one of them or up to three more where that is less for the
-// busiest block (an item counted as a row more than it has).  Cut into so many that every block had at least one, 16 gates of 1024 rows
-// were 160 items for 148 blocks, and twelve blocks had two (4096 columns, fp32 / bf16, us so and as here: backward 330 and 198, forward 204 and
-// 140; 8 gates of 2048 backward 345 and 203, 100 of 164 rows 305 and 257).
+// busiest block.  An item costs a row beside its own, backwards three and a half: the ring drains, and sums are left (16384 x 4096 in items of
+// eight rows 148 and 267 us, of one row 255 and 800, of many 139 and 197).  Cut into so many that every block had at least one, 16 gates of 1024 rows
+// were 160 items for 148 blocks, and twelve blocks had two (4096 columns, fp32 / bf16, us so and as here: backward 330 and 204, forward 204 and
+// 140; 8 gates of 2048 backward 345 and 206, 100 of 164 rows 305 and 256).  Backwards (`sums`) the parts of a cut gate are added up by
+// join_sum_kernel, whose blocks take about a row's time for 128 columns of a gate each, two to an SM: 949 gates of 8 rows of 1312 columns in fp32 are 65 us
+// whole and 188 us in halves.
 struct JoinCut { JoinItems it; int64_t blocks; };
-static inline JoinCut join_cut(const qbp_resnorm_desc *d, const JoinShape &s, bool per_gate, int64_t most, int64_t few)
+static inline JoinCut join_cut(const qbp_resnorm_desc *d, const JoinShape &s, bool per_gate, int64_t most, int64_t few, bool sums)
 {
     JoinCut c{};
     JoinItems &it = c.it;
@@ -412,11 +415,19 @@ static inline JoinCut join_cut(const qbp_resnorm_desc *d, const JoinShape &s, bo
     it.gates = std::max<int64_t>((d->rows + it.gate_rows - 1) / it.gate_rows, 1);
     const auto parts = [](int64_t n, int64_t of) { return (n + of - 1) / of; };
     const int64_t at_once = s.warp ? kJoinWarpRows : 1;              // a block takes so many rows at a time
+    const int64_t beside = sums ? 7 : 2;                             // (in half rows, as the cost and `adding`)
+    const int64_t adding = sums && it.gates > 1 ? 2 * (it.gates * parts(d->cols, 128) / (2 * sm_count())) : 0;
+    const int64_t last_gate = it.rows - (it.gates - 1) * it.gate_rows;         // its rows, maybe fewer than the others'
     int64_t best = std::numeric_limits<int64_t>::max();
-    for (int64_t rounds = parts(it.gates, most), last = rounds + 3; rounds <= last; ++rounds) {
-        const int64_t rows = parts(it.gate_rows, std::min(rounds * most / it.gates, parts(it.gate_rows, few * at_once))), splits = parts(it.gate_rows, rows);
-        const int64_t cost = parts(it.gates * splits, most) * (parts(rows, at_once) + 1);
-        if (cost < best) { best = cost; it.split_rows = rows; it.splits = splits; }
+    const auto consider = [&](int64_t splits) {
+        const int64_t rows = parts(it.gate_rows, std::min(std::max<int64_t>(splits, 1), parts(it.gate_rows, few * at_once))), items = (it.gates - 1) * parts(it.gate_rows, rows) + parts(last_gate, rows);
+        const int64_t cost = parts(items, most) * (2 * parts(rows, at_once) + beside) + (rows < it.gate_rows ? adding : 0);
+        if (cost < best) { best = cost; it.split_rows = rows; it.splits = parts(it.gate_rows, rows); }
+    };
+    for (int64_t rounds = parts(it.gates, most), end = rounds + 4; rounds < end; ++rounds) {
+        const int64_t splits = rounds * most * it.gate_rows / std::max<int64_t>(it.rows, 1);
+        consider(splits);
+        consider(splits - 1);                                        // (the last gate's may be one too many)
     }
     c.blocks = std::min(most, it.gates * it.splits);
     return c;

@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(32 * kSumHigh) join_sum_kernel(const __grid_co
 static size_t gate_parts(const JoinItems &it) { return it.splits > 1 ? (size_t)(it.gates * it.splits * it.cols) : 0; }
 static JoinCut join_cut_bwd(const qbp_resnorm_desc *d, const JoinShape &s, bool per_gate)
 {
-    return join_cut(d, s, per_gate, join_blocks(d, s, 2), s.warp ? 2 : 4);
+    return join_cut(d, s, per_gate, join_blocks(d, s, 2), s.warp ? 2 : 4, true);
 }
 
 extern "C" __attribute__((visibility("default"))) size_t qbp_resnorm_bwd_workspace_bytes(const qbp_resnorm_desc *d)
