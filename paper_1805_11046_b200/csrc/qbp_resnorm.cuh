@@ -418,17 +418,20 @@ static inline JoinCut join_cut(const qbp_resnorm_desc *d, const JoinShape &s, bo
     const int64_t beside = sums ? 7 : 2;                             // (in half rows, as the cost and `adding`)
     const int64_t adding = sums && it.gates > 1 ? 2 * (it.gates * parts(d->cols, 128) / (2 * sm_count())) : 0;
     const int64_t last_gate = it.rows - (it.gates - 1) * it.gate_rows;         // its rows, maybe fewer than the others'
+    const int64_t finest = parts(it.gate_rows, few * at_once);
     int64_t best = std::numeric_limits<int64_t>::max();
     const auto consider = [&](int64_t splits) {
-        const int64_t rows = parts(it.gate_rows, std::min(std::max<int64_t>(splits, 1), parts(it.gate_rows, few * at_once))), items = (it.gates - 1) * parts(it.gate_rows, rows) + parts(last_gate, rows);
-        const int64_t cost = parts(items, most) * (2 * parts(rows, at_once) + beside) + (rows < it.gate_rows ? adding : 0);
-        if (cost < best) { best = cost; it.split_rows = rows; it.splits = parts(it.gate_rows, rows); }
+        const int64_t rows = parts(it.gate_rows, std::min(std::max<int64_t>(splits, 1), finest)), whole = parts(it.gate_rows, rows);
+        const int64_t cost = parts((it.gates - 1) * whole + parts(last_gate, rows), most) * (2 * parts(rows, at_once) + beside) + (whole > 1 ? adding : 0);
+        if (cost < best) { best = cost; it.split_rows = rows; it.splits = whole; }
     };
-    for (int64_t rounds = parts(it.gates, most), end = rounds + 4; rounds < end; ++rounds) {
-        const int64_t splits = rounds * most * it.gate_rows / std::max<int64_t>(it.rows, 1);
-        consider(splits);
-        consider(splits - 1);                                        // (the last gate's may be one too many)
-    }
+    if (it.gates == 1) consider(most);                               // (more rounds only add to it)
+    else
+        for (int64_t rounds = parts(it.gates, most), end = rounds + 4, splits = 0; rounds < end && splits <= finest; ++rounds) {
+            splits = rounds * most * it.gate_rows / it.rows;
+            consider(splits);
+            consider(splits - 1);                                    // (the last gate's may be one too many)
+        }
     c.blocks = std::min(most, it.gates * it.splits);
     return c;
 }

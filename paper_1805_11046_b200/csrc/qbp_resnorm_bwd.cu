@@ -402,11 +402,14 @@ extern "C" __attribute__((visibility("default"))) size_t qbp_resnorm_bwd_workspa
 {
     if (!d || !join_extents_ok(d) || d->rows == 0 || d->cols == 0) return 256;
     size_t most = 0;
-    for (bool vec : {false, true})
-        for (bool per_gate : {false, true}) {
-            const JoinCut c = join_cut_bwd(d, join_shape(d, 2, vec), per_gate);
-            most = std::max(most, 2 * align_up((size_t)(c.blocks * d->cols) * 4, 256) + align_up(gate_parts(c.it) * 4, 256));
-        }
+    // (with and without a gate, rows on the 16-byte boundaries and off them, as far as these are cut differently)
+    const JoinShape off = join_shape(d, 2, false), on = join_shape(d, 2, true);
+    const bool gates = join_gate_rows(d) < d->rows, both = d->cols % 8 == 0 && (on.ch != off.ch || join_blocks(d, on, 2) != join_blocks(d, off, 2));
+    for (int k = 0; k < 4; ++k) {
+        if (((k & 1) && !gates) || ((k & 2) && !both)) continue;
+        const JoinCut c = join_cut_bwd(d, k & 2 ? on : off, (k & 1) != 0);
+        most = std::max(most, 2 * align_up((size_t)(c.blocks * d->cols) * 4, 256) + align_up(gate_parts(c.it) * 4, 256));
+    }
     return 256 + most;
 }
 

@@ -63,3 +63,47 @@ def test_the_widest_rows_with_a_ring(shape):
     assert ring(8192, 0, 0, 1, 0) and ring(8192, 0, 0, 1, 1)
     assert ring(6400, 0, 0, 2, 1) and not ring(6408, 0, 0, 2, 1)
     assert ring(6396, 0, 0, 2, 0) and not ring(6397, 0, 0, 2, 0)
+
+
+WORKSPACES = r"""
+#include "qbp_resnorm.cuh"
+#include <cstdio>
+namespace qbp { int fail(int status, const char *, ...) { return status; } int sm_count() { return 148; } }
+int main()
+{
+    qbp_resnorm_desc d{};
+    long long rows, cols, gate_rows;
+    int x, b;
+    while (scanf("%lld %lld %lld %d %d", &rows, &cols, &gate_rows, &x, &b) == 5) {
+        d.rows = rows; d.cols = cols; d.gate_rows = gate_rows; d.x_dtype = x; d.b_dtype = b;
+        size_t most = 0;
+        for (bool vec : {false, true})
+            for (bool per_gate : {false, true}) {
+                const qbp::JoinShape s = qbp::join_shape(&d, 2, vec);
+                const qbp::JoinCut c = qbp::join_cut(&d, s, per_gate, qbp::join_blocks(&d, s, 2), s.warp ? 2 : 4, true);
+                const size_t row = (size_t)d.cols * 4, blocks = (size_t)c.blocks * row, parts = c.it.splits > 1 ? (size_t)(c.it.gates * c.it.splits) * row : 0;
+                most = std::max(most, 2 * ((blocks + 255) / 256 * 256) + (parts + 255) / 256 * 256);
+            }
+        printf("%zu\n", 256 + most);
+    }
+    return 0;
+}
+"""
+
+
+def test_a_backward_pass_asks_for_the_workspace_of_every_way_it_may_be_cut(tmp_path):
+    """With and without a gate, on the 16-byte boundaries and off them: the call does not know which when it is asked for the size."""
+    import ctypes as C
+    import random
+
+    from paper_1805_11046_b200 import binding as B
+    (tmp_path / "ws.cu").write_text(WORKSPACES)
+    subprocess.run(["/usr/local/cuda/bin/nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-I", str(CSRC), str(tmp_path / "ws.cu"), "-o", str(tmp_path / "ws")], check=True)
+    r = random.Random(3)
+    cases = [(r.randint(1, 40000), r.choice([r.randint(1, 16384), 8 * r.randint(1, 2048), 8 * r.randint(800, 801)]), r.choice([0, 1, 7, 100, 5000, r.randint(1, 40000), 1 << 50]),
+              r.randint(0, 2), r.randint(0, 2)) for _ in range(4000)]
+    got = subprocess.run([str(tmp_path / "ws")], input="\n".join(" ".join(str(v) for v in c) for c in cases), capture_output=True, text=True)
+    assert got.returncode == 0, got
+    for (rows, cols, gate_rows, x, b), need in zip(cases, got.stdout.split()):
+        d = B.ResnormDesc(rows, cols, x, b, 1, 1, 1e-6, 1.0, gate_rows, 0.0, 0, 0, 0)
+        assert B.lib.qbp_resnorm_bwd_workspace_bytes(C.addressof(d)) == int(need), (rows, cols, gate_rows, x, b)
